@@ -425,6 +425,180 @@ d2moe_status d2moe_moe_forward_streamed(
     void* stream, void* io_stream, void* const* events);
 
 /*
+ * The rest of a decoder block's decode step.  The decoders the paper
+ * evaluates (Mixtral-8x7B, LLaMA-MoE, Sec. 5.1) put attention before every
+ * MoE layer; the entry points below run that part beside the layer: the
+ * projections as linear layers with 4-bit weights, the paged key-value cache
+ * with its writer and the attention of one new token per sequence that reads
+ * it, and the norms around a block.  They serve (no backward pass).
+ */
+
+/*
+ * A linear layer's weights in 4 bits with group scales: row r, column c is
+ *     W[r][c] = scale[r][c / group] * (code[r][c] - zero[r][c / group]),
+ * codes and zero points in 0..15.  group is 32, 64 or 128, cols % group == 0,
+ * rows >= 1.  Stored in blocks of 16 rows by 128 columns, RB = ceil(rows/16)
+ * block rows of KB = ceil(cols/128) blocks; what lies past the last row or
+ * column is zero (codes, scales and zeros):
+ *   codes  [RB][KB][64][4] uint32: word j of lane l holds row 16 rb + l % 16,
+ *          columns 128 kb + 32 j + 8 (l / 16) + e, e = 0..7, with code e at
+ *          bits 4 (e / 2 + 4 (e % 2)) .. + 3;
+ *   scales [RB][KB][128/group][16] binary16;
+ *   zeros  [RB][KB][128/group][16] uint8.
+ * All three are device buffers of the sizes reported by d2moe_linear_size,
+ * 16-byte aligned.
+ */
+typedef struct {
+  int32_t rows, cols, group;
+  uint32_t* codes;
+  uint16_t* scales;
+  uint8_t* zeros;
+} d2moe_linear;
+
+d2moe_status d2moe_linear_size(int32_t rows, int32_t cols, int32_t group, size_t* codes_bytes,
+                               size_t* scales_bytes, size_t* zeros_bytes);
+
+/*
+ * Quantize + pack W (device [rows][cols] binary32) into `out`: the base level
+ * of d2moe_pack_mwq (Eq. 2) at four bits, the same binary32 arithmetic:
+ * scale = binary16 of (max(0, max W) - min(0, min W)) / 15 over the group (1
+ * if that is 0 or overflows), zero = rint(-min / scale) clamped, code =
+ * clamp(rint(W / scale + zero)); a NaN weight takes code 0.
+ */
+d2moe_status d2moe_linear_pack(const void* W, d2moe_dtype w_dtype, const d2moe_linear* out,
+                               void* stream);
+
+/*
+ * Pack weights that are quantized already: codes device [rows][cols] uint8,
+ * scales device [rows][cols/group] binary16, zeros device [rows][cols/group]
+ * uint8 or NULL (all 8).  Only the low four bits of codes and zeros are used.
+ */
+d2moe_status d2moe_linear_pack_codes(const uint8_t* codes, const uint16_t* scales,
+                                     const uint8_t* zeros, const d2moe_linear* out,
+                                     void* stream);
+
+/*
+ * y[t][r] = sum_c W[r][c] x[t][c] (+ bias[r]) for T tokens.
+ *   x:    device [T][cols] (x_dtype), 16-byte aligned
+ *   bias: device [rows] float or NULL
+ *   y:    device [T][rows] (y_dtype); bf16 is rounded to nearest even
+ * Products are exact and summed in binary32 within a group, groups in
+ * binary32.  A token with an infinity or NaN among its activations gets NaN or
+ * infinite results; other tokens' do not depend on it.  Any T >= 0; made for
+ * the T of a decode step: above 64 tokens the weights are read again for
+ * every 64.  No workspace; results do not depend on what else runs.
+ */
+d2moe_status d2moe_linear_forward(const void* x, d2moe_dtype x_dtype, int32_t T,
+                                  const d2moe_linear* w, const float* bias, void* y,
+                                  d2moe_dtype y_dtype, void* stream);
+
+/*
+ * A paged key-value cache: n_pages pages of page_size tokens, n_heads key
+ * heads of head_dim values, in one buffer for keys and one for values
+ * (`dtype` both).  The row of (page, token, head) starts page * page_stride +
+ * token * token_stride + head * head_stride elements after the buffer's
+ * start, so [page][token][head][dim], [page][head][token][dim] and halves of
+ * one joint buffer all fit.  head_dim is a multiple of 8, 8..256; buffers are
+ * 16-byte aligned and strides multiples of 16 bytes; rows must not overlap.
+ * A sequence's tokens are found through its row of a block table, device
+ * [n_seqs][max_pages] int32: token p lies in page table[seq][p / page_size]
+ * at p % page_size.
+ */
+typedef struct {
+  int32_t n_pages, page_size, n_heads, head_dim;
+  d2moe_dtype dtype;
+  int64_t page_stride, token_stride, head_stride;
+  void* k;
+  void* v;
+} d2moe_kv_cache;
+
+/*
+ * New tokens into the cache, with the rotary rotation of their queries and
+ * keys.  Token t of N belongs to sequence token_seq[t] (t itself when
+ * token_seq is NULL) at position positions[t]:
+ *     k row, v row of the token -> the cache, at its position;
+ *     q row -> q_out;
+ * q and k rotated when cos and sin are given, values i and i + head_dim/2 of
+ * a head together: (a, b) -> (a cos_i - b sin_i, b cos_i + a sin_i) with
+ * cos_i = cos[position][i].  The arithmetic is binary32, rounded once to the
+ * cache's type.
+ *   q:  device, q_heads rows of head_dim per token, tokens q_stride elements
+ *       apart, or NULL (no queries; q_heads, q_out are then ignored)
+ *   k, v: device, cache->n_heads rows of head_dim per token, kv_stride apart
+ *   block_table: device [n_seqs][max_pages] int32
+ *   positions: device [N] int32; token_seq: device [N] int32 or NULL
+ *   cos, sin: device [n_rot][head_dim/2] float, both or neither
+ *   q_out: device [N][q_heads][head_dim] of the cache's type; may be q when
+ *       q is packed and of that type
+ * x_dtype is the type of q, k and v; they, q_out, cos and sin are 16-byte
+ * aligned, strides multiples of 16 bytes.  A token whose position is
+ * negative, beyond the table's row or (rotated) at n_rot or later, whose
+ * sequence is outside [0, n_seqs) or whose page is outside [0, n_pages) is
+ * not written to the cache; its q row goes to q_out unrotated when its
+ * position is outside [0, n_rot), rotated otherwise.  No two tokens of a call
+ * may share a place in the cache.
+ */
+d2moe_status d2moe_kv_append(const void* q, int64_t q_stride, int32_t q_heads, const void* k,
+                             const void* v, int64_t kv_stride, d2moe_dtype x_dtype, int32_t N,
+                             const d2moe_kv_cache* cache, const int32_t* block_table,
+                             int32_t n_seqs, int32_t max_pages, const int32_t* positions,
+                             const int32_t* token_seq, const float* cos, const float* sin,
+                             int32_t n_rot, void* q_out, void* stream);
+
+/*
+ * Attention of one new token per sequence over the paged cache:
+ *     out[b][h] = sum_j softmax_j(scale q[b][h] . K_j) V_j,
+ * j over the sequence's tokens max(0, n - window) .. n - 1, n = lengths[b]
+ * (window 0: all of them; the new token's own key is among them once it was
+ * appended), K_j, V_j of key head h / (q_heads / n_heads).
+ *   q:   device [B][q_heads][head_dim] of the cache's type, sequences
+ *        q_stride elements apart, 16-byte aligned
+ *   block_table: device [B][max_pages] int32; lengths: device [B] int32
+ *   out: device [B][q_heads][head_dim] of the cache's type
+ *   max_len: host, the largest length expected; only the division of the work
+ *        goes by it, any length gives its result
+ *   workspace: at least d2moe_attn_decode_workspace bytes for this max_len or
+ *        a larger one, 16-byte aligned, or NULL when that says 0; contents need
+ *        no initialisation; calls that may run at the same time need one each
+ * q_heads is a multiple of n_heads; scale is finite.  A sequence of length 0
+ * (or less) gives zeros; a length beyond the table's row counts as the row's
+ * end; a token whose page is outside [0, n_pages) counts as masked, and a row
+ * with every token masked gives zeros.  Cache rows outside the tokens
+ * attended are not used, whatever they hold.  Scores, softmax and sums are
+ * binary32; with a bf16 cache the probabilities enter the value product as
+ * two bf16 terms.
+ */
+d2moe_status d2moe_attn_decode_workspace(int32_t B, int32_t q_heads, int32_t n_heads,
+                                         int32_t head_dim, int32_t max_len, size_t* bytes);
+d2moe_status d2moe_attn_decode(const void* q, int64_t q_stride, int32_t B, int32_t q_heads,
+                               const d2moe_kv_cache* cache, const int32_t* block_table,
+                               int32_t max_pages, const int32_t* lengths, int32_t max_len,
+                               int32_t window, float scale, void* out, void* workspace,
+                               size_t ws_bytes, void* stream);
+
+/*
+ * The norms after a block and before the next one, with the block's gate and
+ * the residual's scales; d2moe_residual_rmsnorm with all of its parts:
+ *     u    = post_w * y[t] / sqrt(mean_c y[t][c]^2 + eps)   (y[t] when
+ *                                                            post_w is NULL)
+ *     x[t] = x_scale * x[t] + y_scale * gate[t] * u         (in place)
+ *     h[t] = pre_w * x[t] / sqrt(mean_c x[t][c]^2 + eps)
+ *   x: device [T][d] float; y: device [T][d] (y_dtype)
+ *   post_w, pre_w: device [d] float or NULL (pre_w NULL: ones)
+ *   gate: device (gate_dtype), token t's row gate_stride * t elements from
+ *        the start (gate_stride 0: one row for all tokens), or NULL (ones)
+ *   h: device [T][d] (h_dtype; bf16 is rounded to nearest even), or NULL
+ *        (only x is updated)
+ * 1 <= d <= 16384, T >= 0, eps >= 0, gate_stride 0 or >= d.  Accumulation is
+ * fp32.
+ */
+d2moe_status d2moe_block_norm(float* x, float x_scale, const void* y, d2moe_dtype y_dtype,
+                              float y_scale, const float* post_w, const void* gate,
+                              d2moe_dtype gate_dtype, int64_t gate_stride, const float* pre_w,
+                              int32_t T, int32_t d, float eps, void* h, d2moe_dtype h_dtype,
+                              void* stream);
+
+/*
  * Measurement helper (not part of the layer): reads `bytes` of device memory
  * at `buf` once with 16-byte nontemporal loads in a grid-stride loop over
  * `blocks` workgroups of 256 threads and writes one XOR word per workgroup to

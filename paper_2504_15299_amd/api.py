@@ -38,6 +38,17 @@ class _BudgetAction(ctypes.Structure):
     _fields_ = [("action", _I), ("layer", _I), ("expert", _I), ("level", _I)]
 
 
+class _Linear(ctypes.Structure):
+    _fields_ = [("rows", _I), ("cols", _I), ("group", _I), ("codes", _P), ("scales", _P),
+                ("zeros", _P)]
+
+
+class _KVCache(ctypes.Structure):
+    _fields_ = [("n_pages", _I), ("page_size", _I), ("n_heads", _I), ("head_dim", _I),
+                ("dtype", _I), ("page_stride", ctypes.c_int64), ("token_stride", ctypes.c_int64),
+                ("head_stride", ctypes.c_int64), ("k", _P), ("v", _P)]
+
+
 class _Routing(ctypes.Structure):
     _fields_ = [("logits", _P), ("topk_idx", _P), ("topk_w", _P), ("topk_bits", _P),
                 ("hist", _P), ("offsets", _P), ("perm", _P), ("slot_of", _P),
@@ -88,7 +99,23 @@ def lib():
             ctypes.POINTER(_Mwq), ctypes.POINTER(_Mwq), _P, ctypes.POINTER(_Routing), _P, _P, _I,
             _P, _P, ctypes.c_size_t, _P, _P, _P]
         L.d2moe_residual_rmsnorm.argtypes = [_P, _P, _I, _I, _I, ctypes.c_float, _P, _I, _P]
-        for name in ("d2moe_mwq_size", "d2moe_pack_mwq", "d2moe_debug_unpack", "d2moe_route",
+        i64, f32, size = ctypes.c_int64, ctypes.c_float, ctypes.c_size_t
+        lin, kvc = ctypes.POINTER(_Linear), ctypes.POINTER(_KVCache)
+        L.d2moe_linear_size.argtypes = [_I, _I, _I, sz, sz, sz]
+        L.d2moe_linear_pack.argtypes = [_P, _I, lin, _P]
+        L.d2moe_linear_pack_codes.argtypes = [_P, _P, _P, lin, _P]
+        L.d2moe_linear_forward.argtypes = [_P, _I, _I, lin, _P, _P, _I, _P]
+        L.d2moe_kv_append.argtypes = [_P, i64, _I, _P, _P, i64, _I, _I, kvc, _P, _I, _I, _P, _P,
+                                      _P, _P, _I, _P, _P]
+        L.d2moe_attn_decode_workspace.argtypes = [_I, _I, _I, _I, _I, sz]
+        L.d2moe_attn_decode.argtypes = [_P, i64, _I, _I, kvc, _P, _I, _P, _I, _I, f32, _P, _P,
+                                        size, _P]
+        L.d2moe_block_norm.argtypes = [_P, f32, _P, _I, f32, _P, _P, _I, i64, _P, _I, _I, f32, _P,
+                                       _I, _P]
+        for name in ("d2moe_linear_size", "d2moe_linear_pack", "d2moe_linear_pack_codes",
+                     "d2moe_linear_forward", "d2moe_kv_append", "d2moe_attn_decode_workspace",
+                     "d2moe_attn_decode", "d2moe_block_norm",
+                     "d2moe_mwq_size", "d2moe_pack_mwq", "d2moe_debug_unpack", "d2moe_route",
                      "d2moe_mwq_calib_factor_workspace", "d2moe_mwq_calib_factor",
                      "d2moe_pack_mwq_calibrated_workspace", "d2moe_pack_mwq_calibrated",
                      "d2moe_route_learned",
@@ -387,6 +414,239 @@ def residual_rmsnorm(x: torch.Tensor, y: torch.Tensor | None, eps: float = 1e-5,
            lib().d2moe_residual_rmsnorm(_ptr(x), _ptr(y) if y is not None else None,
                                         _dtype_code(y) if y is not None else D2MOE_F32, T, d,
                                         float(eps), _ptr(h), _dtype_code(h), _stream(stream)))
+    return h
+
+
+# ---- the rest of a decoder block: 4-bit linear layers, paged cache, norms ------
+
+def _f32(t, shape, dev, what, dtype=torch.float32):
+    """Pointer of an optional contiguous tensor of this shape and type."""
+    if t is None:
+        return None
+    if t.dtype != dtype or tuple(t.shape) != shape or t.device != dev or not t.is_contiguous():
+        raise ValueError(f"{what} must be a contiguous {dtype} tensor of shape {shape} on {dev}")
+    return t.data_ptr()
+
+
+def _i32(t, shape, dev, what):
+    return _f32(t, shape, dev, what, torch.int32)
+
+
+def _new(shape, dtype, dev, stream):
+    """A tensor for a call on ``stream`` (None: the current one)."""
+    t = torch.empty(shape, dtype=dtype, device=dev)
+    if stream is not None:
+        t.record_stream(stream)
+    return t
+
+
+def _run(name, dev, stream, *args):
+    """The entry point on ``stream`` (None: the current one of the tensors'
+    device), with that device current."""
+    if dev.type != "cuda":
+        raise ValueError(f"{name}: tensors must be on a GPU, not on {dev}")
+    if stream is None:
+        stream = torch.cuda.current_stream(dev)
+    fn = getattr(lib(), name)
+    if dev.index == torch.cuda.current_device():
+        rc = fn(*args, stream.cuda_stream)
+    else:
+        with torch.cuda.device(dev):
+            rc = fn(*args, stream.cuda_stream)
+    if rc != OK:
+        raise D2MoEError(name, rc)
+
+
+def linear_size(rows, cols, group=128):
+    a, b, c = ctypes.c_size_t(), ctypes.c_size_t(), ctypes.c_size_t()
+    _check("d2moe_linear_size", lib().d2moe_linear_size(rows, cols, group, ctypes.byref(a),
+                                                        ctypes.byref(b), ctypes.byref(c)))
+    return a.value, b.value, c.value
+
+
+class Linear:
+    """Device buffers of a linear layer's 4-bit weights (``d2moe_linear``)."""
+
+    def __init__(self, rows, cols, group, codes, scales, zeros):
+        sizes = linear_size(rows, cols, group)
+        for t, n in zip((codes, scales, zeros), sizes):
+            if t.numel() * t.element_size() != n or not t.is_contiguous() or \
+                    t.device != codes.device:
+                raise ValueError(f"buffers of {sizes} bytes on one device are needed")
+        self.rows, self.cols, self.group = rows, cols, group
+        self.codes, self.scales, self.zeros = codes, scales, zeros
+        self._c = _Linear(rows, cols, group, codes.data_ptr(), scales.data_ptr(),
+                          zeros.data_ptr())
+
+    @staticmethod
+    def empty(rows, cols, group=128, device="cuda"):
+        cb, sb, zb = linear_size(rows, cols, group)
+        return Linear(rows, cols, group, torch.empty(cb // 4, dtype=torch.int32, device=device),
+                      torch.empty(sb // 2, dtype=torch.int16, device=device),
+                      torch.empty(zb, dtype=torch.uint8, device=device))
+
+    def nbytes(self):
+        return self.codes.numel() * 4 + self.scales.numel() * 2 + self.zeros.numel()
+
+
+def linear_pack(W: torch.Tensor, out: Linear, stream=None) -> Linear:
+    """``d2moe_linear_pack``: quantize + pack W [rows][cols] (fp32, device)."""
+    dev = out.codes.device
+    _run("d2moe_linear_pack", dev, stream, _f32(W, (out.rows, out.cols), dev, "W"), D2MOE_F32,
+         ctypes.byref(out._c))
+    return out
+
+
+def linear_pack_codes(codes: torch.Tensor, scales: torch.Tensor, zeros, out: Linear,
+                      stream=None) -> Linear:
+    """``d2moe_linear_pack_codes``: codes [rows][cols] uint8 (0..15), scales
+    [rows][cols/group] float16, zeros [rows][cols/group] uint8 or None (8)."""
+    dev, g = out.codes.device, (out.rows, out.cols // out.group)
+    _run("d2moe_linear_pack_codes", dev, stream,
+         _f32(codes, (out.rows, out.cols), dev, "codes", torch.uint8),
+         _f32(scales, g, dev, "scales", torch.float16), _f32(zeros, g, dev, "zeros", torch.uint8),
+         ctypes.byref(out._c))
+    return out
+
+
+def linear_forward(x: torch.Tensor, w: Linear, bias: torch.Tensor | None = None,
+                   y: torch.Tensor | None = None, y_dtype=None, stream=None) -> torch.Tensor:
+    """``d2moe_linear_forward``: x [T][cols] -> [T][rows] (y_dtype, x's type
+    when not given); bias [rows] float32 or None."""
+    T, dev = x.shape[0], w.codes.device
+    px = _f32(x, (T, w.cols), dev, "x", x.dtype)
+    if y is None:
+        y = _new((T, w.rows), x.dtype if y_dtype is None else y_dtype, dev, stream)
+    _run("d2moe_linear_forward", dev, stream, px, _dtype_code(x), T, ctypes.byref(w._c),
+         _f32(bias, (w.rows,), dev, "bias"), _f32(y, (T, w.rows), dev, "y", y.dtype),
+         _dtype_code(y))
+    return y
+
+
+class KVCache:
+    """A paged key-value cache over two tensors [page][token][head][dim] of
+    one shape and one set of strides (``d2moe_kv_cache``); views of another
+    order or of a joint buffer will do."""
+
+    def __init__(self, k: torch.Tensor, v: torch.Tensor):
+        if k.dim() != 4 or k.shape != v.shape or k.stride() != v.stride() or \
+                k.dtype != v.dtype or k.device != v.device or k.stride(3) != 1:
+            raise ValueError("k and v must be [page][token][head][dim] tensors of one type, shape "
+                             "and stride, dim contiguous")
+        self.k, self.v = k, v
+        self.n_pages, self.page_size, self.n_heads, self.head_dim = k.shape
+        self._c = _KVCache(*k.shape, _dtype_code(k), *k.stride()[:3], k.data_ptr(), v.data_ptr())
+
+    @staticmethod
+    def empty(n_pages, page_size, n_heads, head_dim, dtype=torch.bfloat16, device="cuda"):
+        shape = (n_pages, page_size, n_heads, head_dim)
+        return KVCache(torch.empty(shape, dtype=dtype, device=device),
+                       torch.empty(shape, dtype=dtype, device=device))
+
+
+def _rows(t, heads, dim, dev, what):
+    """Pointer and token stride of a [token][head][dim] tensor whose heads are
+    packed."""
+    if t.dim() != 3 or tuple(t.shape[1:]) != (heads, dim) or t.device != dev or \
+            t.stride(2) != 1 or (heads > 1 and t.stride(1) != dim):
+        raise ValueError(f"{what} must be a [token][{heads}][{dim}] tensor on {dev}, heads packed")
+    return t.data_ptr(), t.stride(0) if t.shape[0] > 1 else heads * dim
+
+
+def kv_append(q, k: torch.Tensor, v: torch.Tensor, cache: KVCache, block_table: torch.Tensor,
+              positions: torch.Tensor, token_seq: torch.Tensor | None = None, cos=None, sin=None,
+              q_out: torch.Tensor | None = None, stream=None):
+    """``d2moe_kv_append``: q [N][q_heads][dim] or None, k and v
+    [N][heads][dim] (views with packed heads will do), block_table
+    [n_seqs][max_pages], positions [N] and token_seq [N] int32, cos and sin
+    [n_rot][dim/2] float32.  Returns q_out [N][q_heads][dim] of the cache's
+    type (None without q)."""
+    dev, N, D = cache.k.device, k.shape[0], cache.head_dim
+    pk, ks = _rows(k, cache.n_heads, D, dev, "k")
+    pv, vs = _rows(v, cache.n_heads, D, dev, "v")
+    if v.shape[0] != N or v.dtype != k.dtype or (N > 1 and vs != ks):
+        raise ValueError("v must match k")
+    pq, qs, heads, po = None, 0, 0, None
+    if q is not None:
+        heads = q.shape[1]
+        pq, qs = _rows(q, heads, D, dev, "q")
+        if q.shape[0] != N or q.dtype != k.dtype:
+            raise ValueError("q must match k")
+        if q_out is None:
+            q_out = _new((N, heads, D), cache.k.dtype, dev, stream)
+        po = _f32(q_out, (N, heads, D), dev, "q_out", cache.k.dtype)
+    n_seqs, pages = block_table.shape
+    n_rot = 0 if cos is None else cos.shape[0]
+    _run("d2moe_kv_append", dev, stream, pq, qs, heads, pk, pv, ks, _dtype_code(k), N,
+         ctypes.byref(cache._c), _i32(block_table, (n_seqs, pages), dev, "block_table"), n_seqs,
+         pages, _i32(positions, (N,), dev, "positions"), _i32(token_seq, (N,), dev, "token_seq"),
+         _f32(cos, (n_rot, D // 2), dev, "cos"), _f32(sin, (n_rot, D // 2), dev, "sin"), n_rot, po)
+    return q_out
+
+
+def attn_decode_workspace(B: int, q_heads: int, cache: KVCache, max_len: int) -> int:
+    n = ctypes.c_size_t()
+    _check("d2moe_attn_decode_workspace",
+           lib().d2moe_attn_decode_workspace(B, q_heads, cache.n_heads, cache.head_dim, max_len,
+                                             ctypes.byref(n)))
+    return n.value
+
+
+def attn_decode(q: torch.Tensor, cache: KVCache, block_table: torch.Tensor, lengths: torch.Tensor,
+                scale: float | None = None, window: int = 0, max_len: int | None = None,
+                out: torch.Tensor | None = None, workspace: torch.Tensor | None = None,
+                stream=None) -> torch.Tensor:
+    """``d2moe_attn_decode``: q [B][q_heads][dim] of the cache's type,
+    block_table [B][max_pages] and lengths [B] int32 (device) -> out
+    [B][q_heads][dim].  ``scale`` is 1 / sqrt(dim) when not given, ``max_len``
+    the length that fills a row of the table."""
+    dev, D = cache.k.device, cache.head_dim
+    if q.dim() != 3 or q.dtype != cache.k.dtype:
+        raise ValueError(f"q must be a [B][q_heads][{D}] tensor of the cache's type")
+    B, heads = q.shape[:2]
+    pq, qs = _rows(q, heads, D, dev, "q")
+    pages = block_table.shape[1]
+    if max_len is None:
+        max_len = min(pages * cache.page_size, 0x7fffffff)
+    if out is None:
+        out = _new((B, heads, D), q.dtype, dev, stream)
+    if workspace is None:
+        need = attn_decode_workspace(B, heads, cache, max_len)
+        workspace = _new((need,), torch.uint8, dev, stream) if need else None
+    elif workspace.device != dev or not workspace.is_contiguous():
+        raise ValueError(f"workspace must be a contiguous tensor on {dev}")
+    _run("d2moe_attn_decode", dev, stream, pq, qs, B, heads, ctypes.byref(cache._c),
+         _i32(block_table, (B, pages), dev, "block_table"), pages,
+         _i32(lengths, (B,), dev, "lengths"), max_len, window,
+         D ** -0.5 if scale is None else float(scale), _f32(out, (B, heads, D), dev, "out", q.dtype),
+         None if workspace is None else workspace.data_ptr(),
+         0 if workspace is None else workspace.numel() * workspace.element_size())
+    return out
+
+
+def block_norm(x: torch.Tensor, y: torch.Tensor, eps: float = 1e-5, pre_weight=None,
+               post_weight=None, gate=None, x_scale: float = 1.0, y_scale: float = 1.0,
+               h: torch.Tensor | None = None, h_dtype=torch.bfloat16, stream=None):
+    """``d2moe_block_norm``: x [T][d] float32, updated in place to
+    x_scale * x + y_scale * gate * postnorm(y); returns h = prenorm(x) (h_dtype;
+    None: only x is updated).  y [T][d]; gate [d] or [T][d] (rows may be
+    strided); pre_weight, post_weight [d] float32 or None."""
+    T, d = x.shape
+    dev = x.device
+    px, py = _f32(x, (T, d), dev, "x"), _f32(y, (T, d), dev, "y", y.dtype)
+    pg, gs, gd = None, 0, D2MOE_F32
+    if gate is not None:
+        if tuple(gate.shape) not in ((d,), (T, d)) or gate.device != dev or \
+                (d > 1 and gate.stride(-1) != 1):
+            raise ValueError(f"gate must be [d] or [T][d] = {(T, d)} on {dev}, rows contiguous")
+        pg, gs, gd = gate.data_ptr(), gate.stride(0) if gate.dim() == 2 else 0, _dtype_code(gate)
+    if h is None and h_dtype is not None:
+        h = _new((T, d), h_dtype, dev, stream)
+    _run("d2moe_block_norm", dev, stream, px, float(x_scale), py, _dtype_code(y), float(y_scale),
+         _f32(post_weight, (d,), dev, "post_weight"), pg, gd, gs,
+         _f32(pre_weight, (d,), dev, "pre_weight"), T, d, float(eps),
+         None if h is None else _f32(h, (T, d), dev, "h", h.dtype),
+         D2MOE_F32 if h is None else _dtype_code(h))
     return h
 
 

@@ -48,7 +48,7 @@ ARCH = "gfx950"
 COMMON = ["-O3", "-fPIC", "-std=c++17", f"--offload-arch={ARCH}", "-I", INCLUDE,
           "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
           "-Wno-unused-command-line-argument"]
-EXTRA = {"pack.hip": ["-ffp-contract=off"], "calib.hip": ["-ffp-contract=off"]}
+EXTRA = {f: ["-ffp-contract=off"] for f in ("pack.hip", "calib.hip", "linear_pack.hip")}
 
 
 def _hipcc() -> str:

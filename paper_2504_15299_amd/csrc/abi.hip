@@ -6,6 +6,7 @@
 #include <mutex>
 #include <vector>
 
+#include "decoder.h"
 #include "internal.h"
 
 using namespace d2moe;
@@ -30,6 +31,44 @@ bool shape_ok(int rows, int cols, int group) {
 bool mwq_ok(const d2moe_mwq* m) {
   return m && m->n_experts >= 1 && shape_ok(m->rows, m->cols, m->group) &&
          ladder_ok(m->b_min, m->b_max) && m->planes && m->scales && m->zeros;
+}
+
+bool aligned(const void* p, size_t to) { return ((uintptr_t)p & (to - 1)) == 0; }
+
+bool dtype_ok(d2moe_dtype t) { return t == D2MOE_F32 || t == D2MOE_BF16; }
+int64_t dtype_size(d2moe_dtype t) { return t == D2MOE_BF16 ? 2 : 4; }
+
+bool linear_shape_ok(int rows, int cols, int group) {
+  return rows >= 1 && (group == 32 || group == 64 || group == 128) && cols >= group &&
+         cols % group == 0 && cols <= (1 << 24);
+}
+
+bool linear_ok(const d2moe_linear* w) {
+  return w && linear_shape_ok(w->rows, w->cols, w->group) && w->codes && w->scales && w->zeros &&
+         aligned(w->codes, 16) && aligned(w->scales, 16) && aligned(w->zeros, 16);
+}
+
+// Sizes, alignment and that no two rows of the cache overlap: of the three
+// strides, each covers what the smaller ones span.
+bool cache_ok(const d2moe_kv_cache* c) {
+  if (!c || !dtype_ok(c->dtype) || c->n_pages < 1 || c->page_size < 1 || c->n_heads < 1 ||
+      c->head_dim < 8 || c->head_dim > 256 || c->head_dim % 8 != 0 || !c->k || !c->v ||
+      !aligned(c->k, 16) || !aligned(c->v, 16))
+    return false;
+  struct Dim {
+    int64_t n, stride;
+  } d[3] = {{c->n_pages, c->page_stride}, {c->page_size, c->token_stride},
+            {c->n_heads, c->head_stride}};
+  std::sort(d, d + 3, [](const Dim& x, const Dim& y) { return x.stride < y.stride; });
+  int64_t span = c->head_dim;
+  for (const Dim& x : d) {
+    if (x.n == 1) continue;  // its stride is never used
+    if (x.stride < span || x.stride % (16 / dtype_size(c->dtype)) != 0 ||
+        x.stride > ((int64_t)1 << 46) / x.n)
+      return false;
+    span += (x.n - 1) * x.stride;
+  }
+  return true;
 }
 
 d2moe_status from_hip(hipError_t e) { return e == hipSuccess ? D2MOE_OK : D2MOE_EHIP; }
@@ -277,6 +316,117 @@ d2moe_status d2moe_residual_rmsnorm(float* x, const void* y, d2moe_dtype y_dtype
   if (T > 0 && (!x || !h)) return D2MOE_EINVAL;
   return from_hip(launch_residual_rmsnorm(x, y, y_dtype, T, d, eps, h, h_dtype,
                                           (hipStream_t)stream));
+}
+
+d2moe_status d2moe_linear_size(int32_t rows, int32_t cols, int32_t group, size_t* codes_bytes,
+                               size_t* scales_bytes, size_t* zeros_bytes) {
+  if (!linear_shape_ok(rows, cols, group)) return D2MOE_EINVAL;
+  const d2moe_linear w{rows, cols, group, nullptr, nullptr, nullptr};
+  const size_t blocks = (size_t)lin_row_blocks(&w) * lin_col_blocks(&w);
+  const size_t groups = blocks * (kLinCols / group) * kLinRows;
+  if (codes_bytes) *codes_bytes = blocks * (kLinRows * kLinCols / 2);
+  if (scales_bytes) *scales_bytes = groups * 2;
+  if (zeros_bytes) *zeros_bytes = groups;
+  return D2MOE_OK;
+}
+
+d2moe_status d2moe_linear_pack(const void* W, d2moe_dtype w_dtype, const d2moe_linear* out,
+                               void* stream) {
+  if (!W || !linear_ok(out)) return D2MOE_EINVAL;
+  if (w_dtype != D2MOE_F32) return D2MOE_EUNSUPPORTED;
+  return from_hip(launch_linear_pack((const float*)W, out, (hipStream_t)stream));
+}
+
+d2moe_status d2moe_linear_pack_codes(const uint8_t* codes, const uint16_t* scales,
+                                     const uint8_t* zeros, const d2moe_linear* out,
+                                     void* stream) {
+  if (!codes || !scales || !linear_ok(out)) return D2MOE_EINVAL;
+  return from_hip(launch_linear_pack_codes(codes, scales, zeros, out, (hipStream_t)stream));
+}
+
+d2moe_status d2moe_linear_forward(const void* x, d2moe_dtype x_dtype, int32_t T,
+                                  const d2moe_linear* w, const float* bias, void* y,
+                                  d2moe_dtype y_dtype, void* stream) {
+  if (T < 0 || T > (1 << 20) || !linear_ok(w)) return D2MOE_EINVAL;
+  if (!dtype_ok(x_dtype) || !dtype_ok(y_dtype)) return D2MOE_EUNSUPPORTED;
+  if (T > 0 && (!x || !y || !aligned(x, 16))) return D2MOE_EINVAL;
+  return from_hip(launch_linear(x, x_dtype, T, w, bias, y, y_dtype, (hipStream_t)stream));
+}
+
+d2moe_status d2moe_kv_append(const void* q, int64_t q_stride, int32_t q_heads, const void* k,
+                             const void* v, int64_t kv_stride, d2moe_dtype x_dtype, int32_t N,
+                             const d2moe_kv_cache* cache, const int32_t* block_table,
+                             int32_t n_seqs, int32_t max_pages, const int32_t* positions,
+                             const int32_t* token_seq, const float* cos, const float* sin,
+                             int32_t n_rot, void* q_out, void* stream) {
+  if (!dtype_ok(x_dtype)) return D2MOE_EUNSUPPORTED;
+  if (N < 0 || !cache_ok(cache) || n_seqs < 0 || max_pages < 0) return D2MOE_EINVAL;
+  if (!cos != !sin || (cos && (n_rot < 0 || !aligned(cos, 16) || !aligned(sin, 16))))
+    return D2MOE_EINVAL;
+  if (N == 0) return D2MOE_OK;
+  const int64_t step = 16 / dtype_size(x_dtype), D = cache->head_dim;
+  if (!k || !v || !positions || !aligned(k, 16) || !aligned(v, 16) || kv_stride % step != 0 ||
+      (N > 1 && kv_stride < cache->n_heads * D) || cache->n_heads > (1 << 16) ||
+      (n_seqs > 0 && max_pages > 0 && !block_table))
+    return D2MOE_EINVAL;
+  if (q && (q_heads < 1 || q_heads > (1 << 16) || !q_out || !aligned(q, 16) ||
+            !aligned(q_out, 16) || q_stride % step != 0 || (N > 1 && q_stride < q_heads * D)))
+    return D2MOE_EINVAL;
+  // in place: the same rows of the same type
+  if (q && q == q_out && (x_dtype != cache->dtype || (N > 1 && q_stride != q_heads * D)))
+    return D2MOE_EINVAL;
+  return from_hip(launch_kv_append(q, q_stride, q_heads, k, v, kv_stride, x_dtype, N, cache,
+                                   block_table, n_seqs, max_pages, positions, token_seq, cos, sin,
+                                   n_rot, q_out, (hipStream_t)stream));
+}
+
+static bool attn_shape_ok(int B, int q_heads, int n_heads, int dim, int max_len) {
+  return B >= 0 && B <= 65535 && n_heads >= 1 && q_heads >= n_heads && q_heads <= 65535 &&
+         q_heads % n_heads == 0 && dim >= 8 && dim <= 256 && dim % 8 == 0 && max_len >= 0;
+}
+
+d2moe_status d2moe_attn_decode_workspace(int32_t B, int32_t q_heads, int32_t n_heads,
+                                         int32_t head_dim, int32_t max_len, size_t* bytes) {
+  if (!attn_shape_ok(B, q_heads, n_heads, head_dim, max_len) || !bytes) return D2MOE_EINVAL;
+  *bytes = attn_decode_workspace(B, q_heads, n_heads, head_dim, max_len);
+  return D2MOE_OK;
+}
+
+d2moe_status d2moe_attn_decode(const void* q, int64_t q_stride, int32_t B, int32_t q_heads,
+                               const d2moe_kv_cache* cache, const int32_t* block_table,
+                               int32_t max_pages, const int32_t* lengths, int32_t max_len,
+                               int32_t window, float scale, void* out, void* workspace,
+                               size_t ws_bytes, void* stream) {
+  if (!cache_ok(cache) ||
+      !attn_shape_ok(B, q_heads, cache->n_heads, cache->head_dim, max_len) || max_pages < 0 ||
+      window < 0 || !(scale - scale == 0.0f))
+    return D2MOE_EINVAL;
+  if (B == 0) return D2MOE_OK;
+  const int64_t step = 16 / dtype_size(cache->dtype);
+  if (!q || !out || !lengths || !aligned(q, 16) || !aligned(out, 16) || q_stride % step != 0 ||
+      (B > 1 && q_stride < (int64_t)q_heads * cache->head_dim) || (max_pages > 0 && !block_table))
+    return D2MOE_EINVAL;
+  const size_t need =
+      attn_decode_workspace(B, q_heads, cache->n_heads, cache->head_dim, max_len);
+  if (need > 0 && (!workspace || ws_bytes < need || !aligned(workspace, 16)))
+    return D2MOE_EWORKSPACE;
+  return from_hip(launch_attn_decode(q, q_stride, B, q_heads, cache, block_table, max_pages,
+                                     lengths, max_len, window, scale, out, workspace,
+                                     (hipStream_t)stream));
+}
+
+d2moe_status d2moe_block_norm(float* x, float x_scale, const void* y, d2moe_dtype y_dtype,
+                              float y_scale, const float* post_w, const void* gate,
+                              d2moe_dtype gate_dtype, int64_t gate_stride, const float* pre_w,
+                              int32_t T, int32_t d, float eps, void* h, d2moe_dtype h_dtype,
+                              void* stream) {
+  if (T < 0 || d < 1 || d > norm_max_cols() || !(eps >= 0.0f)) return D2MOE_EINVAL;
+  if (!dtype_ok(y_dtype) || !dtype_ok(h_dtype) || !dtype_ok(gate_dtype)) return D2MOE_EINVAL;
+  if (gate && gate_stride != 0 && gate_stride < d) return D2MOE_EINVAL;
+  if (T > 0 && (!x || !y)) return D2MOE_EINVAL;
+  return from_hip(launch_block_norm(x, x_scale, y, y_dtype, y_scale, post_w, gate, gate_dtype,
+                                    gate_stride, pre_w, T, d, eps, h, h_dtype,
+                                    (hipStream_t)stream));
 }
 
 d2moe_status d2moe_stream_read(const void* buf, size_t bytes, uint32_t* sink, int32_t blocks,

@@ -1,0 +1,159 @@
+"""New tokens into the paged cache: every written row against binary64 (equal
+where nothing is rotated), every other row left as it was."""
+import numpy as np
+import pytest
+import torch
+
+import decoder_ref as ref
+from layer_cases import DEV
+from paper_2504_15299_amd import api
+
+pytestmark = pytest.mark.gpu
+
+BF, F32 = torch.bfloat16, torch.float32
+
+
+def layout(order, pages, page, H, D, dtype, seed=0):
+    """A cache whose memory has the given order of dimensions."""
+    g = torch.Generator().manual_seed(seed)
+    if order == "joint":                     # [page][k or v][token][head][dim]
+        both = torch.randn((pages, 2, page, H, D), generator=g).to(dtype).to(DEV)
+        return api.KVCache(both[:, 0], both[:, 1])
+    names = {"p": pages, "t": page, "h": H, "d": D}
+    kv = []
+    for _ in range(2):
+        m = torch.randn([names[c] for c in order], generator=g).to(dtype).to(DEV)
+        kv.append(m.permute([order.index(c) for c in "pthd"]))
+    return api.KVCache(*kv)
+
+
+def run(N, seqs, H, Hq, D, page, x_dtype, dtype, rotary, order="pthd", seed=0, in_place=False):
+    rng = np.random.default_rng(seed)
+    width = 4
+    cache = layout(order, seqs * width + 3, page, H, D, dtype, seed)
+    k0, v0 = cache.k.clone(), cache.v.clone()
+    table = rng.permutation(seqs * width + 3)[:seqs * width].reshape(seqs, width).astype(np.int32)
+    # distinct places, in no order
+    spots = rng.permutation(seqs * width * page)[:N]
+    seq, pos = (spots // (width * page)).astype(np.int32), (spots % (width * page)).astype(np.int32)
+    n_rot = width * page
+    cos = sin = None
+    if rotary:
+        ang = np.arange(n_rot)[:, None] / 100.0 ** (np.arange(D // 2) / max(1, D // 2))
+        cos, sin = np.cos(ang).astype(np.float32), np.sin(ang).astype(np.float32)
+    qkv = ref.as_type(rng.standard_normal((N, Hq + 2 * H, D)), x_dtype).to(DEV)
+    q, k, v = qkv[:, :Hq], qkv[:, Hq:Hq + H], qkv[:, Hq + H:]
+    if in_place:
+        q = q.contiguous()
+    dev = lambda a: None if a is None else torch.from_numpy(a).to(DEV)  # noqa: E731
+    q64, k64, v64 = ref.f64(q), ref.f64(k), ref.f64(v)
+    out = api.kv_append(q if Hq else None, k, v, cache, dev(table), dev(pos), dev(seq), dev(cos),
+                        dev(sin), q_out=q if in_place else None)
+    c64 = None if cos is None else cos.astype(np.float64)
+    s64 = None if sin is None else sin.astype(np.float64)
+    at = (torch.from_numpy(table[seq, pos // page].astype(np.int64)),
+          torch.from_numpy((pos % page).astype(np.int64)))
+    kr, ke = ref.kv_append(k64, c64, s64, pos)
+    ref.close(cache.k[at], kr, ke, dtype, "k")
+    ref.close(cache.v[at], v64, np.zeros_like(v64), dtype, "v")
+    if not rotary:
+        assert torch.equal(cache.k[at], k.to(dtype)) and torch.equal(cache.v[at], v.to(dtype))
+    if Hq:
+        qr, qe = ref.kv_append(q64, c64, s64, pos)
+        ref.close(out, qr, qe, dtype, "q")
+    else:
+        assert out is None
+    k0[at], v0[at] = cache.k[at], cache.v[at]
+    assert torch.equal(cache.k, k0) and torch.equal(cache.v, v0)
+
+
+@pytest.mark.parametrize("D", [8, 16, 24, 64, 72, 80, 128, 256])
+@pytest.mark.parametrize("x_dtype,dtype", [(BF, BF), (F32, F32), (F32, BF), (BF, F32)])
+@pytest.mark.parametrize("rotary", [True, False])
+def test_dims_and_types(D, x_dtype, dtype, rotary):
+    run(N=9, seqs=3, H=2, Hq=6, D=D, page=5, x_dtype=x_dtype, dtype=dtype, rotary=rotary)
+
+
+@pytest.mark.parametrize("order", ["pthd", "phtd", "joint", "hptd"])
+@pytest.mark.parametrize("N,page", [(1, 1), (1, 16), (70, 16), (7, 3)])
+def test_orders_and_pages(order, N, page):
+    run(N=N, seqs=5, H=4, Hq=4, D=64, page=page, x_dtype=BF, dtype=BF, rotary=True, order=order,
+        seed=N)
+
+
+def test_heads():
+    run(N=6, seqs=2, H=1, Hq=0, D=64, page=8, x_dtype=BF, dtype=BF, rotary=True)
+    run(N=6, seqs=2, H=1, Hq=1, D=64, page=8, x_dtype=BF, dtype=BF, rotary=True)
+    run(N=6, seqs=2, H=8, Hq=64, D=128, page=8, x_dtype=BF, dtype=BF, rotary=True)
+    run(N=300, seqs=4, H=2, Hq=4, D=64, page=32, x_dtype=BF, dtype=BF, rotary=True)
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+def test_in_place(dtype):
+    run(N=9, seqs=3, H=2, Hq=4, D=64, page=5, x_dtype=dtype, dtype=dtype, rotary=True,
+        in_place=True)
+
+
+@pytest.mark.parametrize("rotary", [True, False])
+def test_tokens_without_a_place_are_skipped(rotary):
+    D, H, page = 16, 2, 4
+    cache = layout("pthd", 6, page, H, D, F32)
+    k0, v0 = cache.k.clone(), cache.v.clone()
+    table = torch.tensor([[0, 7, -1], [6, 2, -2147483648]], dtype=torch.int32, device=DEV)
+    # beyond the row, negative, page 7 of 6, page -1, sequence outside, page 6
+    # of 6, past the rotation's rows, written
+    pos = torch.tensor([12, -1, 5, 9, 0, 0, 0, 11, 6], dtype=torch.int32, device=DEV)
+    seq = torch.tensor([0, 0, 0, 0, 2, -1, 1, 1, 1], dtype=torch.int32, device=DEV)
+    x = torch.randn((9, 3 * H, D), device=DEV)
+    cos = sin = None
+    if rotary:
+        cos, sin = torch.rand((11, D // 2), device=DEV), torch.rand((11, D // 2), device=DEV)
+    out = api.kv_append(x[:, :H], x[:, H:2 * H], x[:, 2 * H:], cache, table, pos, seq, cos, sin)
+    p = pos.cpu().numpy()
+    inside = (p >= 0) & (p < 11)
+    want, err = ref.f64(x[:, :H]), 0 * ref.f64(x[:, :H])
+    if rotary:
+        r, e = ref.kv_append(want[inside], ref.f64(cos), ref.f64(sin), p[inside])
+        want[inside], err[inside] = r, e
+    ref.close(out, want, err, F32)
+    assert not torch.equal(cache.k[2, 2], k0[2, 2])
+    assert torch.equal(cache.v[2, 2], x[8, 2 * H:])
+    k0[2, 2], v0[2, 2] = cache.k[2, 2], cache.v[2, 2]
+    assert torch.equal(cache.k, k0) and torch.equal(cache.v, v0)
+
+
+def test_without_token_seq_token_t_is_of_sequence_t():
+    cache = layout("pthd", 4, 2, 1, 8, BF)
+    table = torch.tensor([[3], [1]], dtype=torch.int32, device=DEV)
+    x = torch.randn((2, 1, 8), device=DEV, dtype=BF)
+    api.kv_append(None, x, x, cache, table, torch.tensor([1, 0], dtype=torch.int32, device=DEV))
+    assert torch.equal(cache.k[3, 1], x[0]) and torch.equal(cache.v[1, 0], x[1])
+
+
+def test_no_tokens():
+    cache = layout("pthd", 4, 2, 1, 8, BF)
+    z = torch.empty((0, 1, 8), device=DEV, dtype=BF)
+    out = api.kv_append(z, z, z, cache, torch.empty((0, 1), dtype=torch.int32, device=DEV),
+                        torch.empty(0, dtype=torch.int32, device=DEV))
+    assert out.shape == (0, 1, 8)
+
+
+def test_rejects_wrong_arguments():
+    cache = layout("pthd", 4, 2, 2, 8, BF)
+    x = torch.zeros((3, 2, 8), device=DEV, dtype=BF)
+    table = torch.zeros((3, 1), dtype=torch.int32, device=DEV)
+    pos = torch.zeros(3, dtype=torch.int32, device=DEV)
+    ok = dict(q=x, k=x, v=x, cache=cache, block_table=table, positions=pos)
+    for bad in (dict(q=x[:2]), dict(k=x[:, :1]), dict(v=x.float()), dict(q=x.float()),
+                dict(positions=pos[:2]), dict(positions=pos.long()), dict(block_table=table.long()),
+                dict(token_seq=pos[:1]), dict(cos=torch.zeros((4, 4), device=DEV),
+                                              sin=torch.zeros((3, 4), device=DEV)),
+                dict(k=x.cpu()), dict(q_out=x[:2])):
+        with pytest.raises(ValueError):
+            api.kv_append(**{**ok, **bad})
+    with pytest.raises(api.D2MoEError) as e:        # one of the two tables only
+        api.kv_append(**ok, cos=torch.zeros((4, 4), device=DEV))
+    assert e.value.status == api.EINVAL
+    wide = torch.zeros((3, 4, 8), device=DEV, dtype=BF)
+    with pytest.raises(ValueError):                 # in place needs packed rows
+        api.kv_append(**{**ok, "q": wide[:, :2], "q_out": wide[:, :2]})

@@ -1,0 +1,151 @@
+"""4-bit linear layers on the GPU: the packed layout and the quantization
+exactly, the product against binary64 within the bound of its arithmetic."""
+import numpy as np
+import pytest
+import torch
+
+import decoder_ref as ref
+from layer_cases import DEV
+from paper_2504_15299_amd import api
+
+pytestmark = pytest.mark.gpu
+
+BF, F32 = torch.bfloat16, torch.float32
+
+
+def weights(rows, cols, group, seed=0):
+    rng = np.random.default_rng(seed)
+    codes = rng.integers(0, 16, (rows, cols), dtype=np.uint8)
+    scales = (rng.random((rows, cols // group)) * 0.01 + 1e-4).astype(np.float16)
+    zeros = rng.integers(0, 16, (rows, cols // group), dtype=np.uint8)
+    return codes, scales, zeros
+
+
+def packed(codes, scales, zeros, group):
+    t = [None if a is None else torch.from_numpy(a).to(DEV) for a in (codes, scales, zeros)]
+    return api.linear_pack_codes(*t, api.Linear.empty(*codes.shape, group, device=DEV))
+
+
+def buffers(w):
+    return (w.codes.cpu().numpy().view(np.uint32), w.scales.cpu().numpy().view(np.float16),
+            w.zeros.cpu().numpy())
+
+
+@pytest.mark.parametrize("rows,cols,group", [(1, 32, 32), (16, 128, 128), (17, 96, 32),
+                                             (100, 192, 64), (33, 640, 128)])
+@pytest.mark.parametrize("given_zeros", [True, False])
+def test_layout_of_given_codes(rows, cols, group, given_zeros):
+    codes, scales, zeros = weights(rows, cols, group)
+    if not given_zeros:
+        zeros[:] = 8
+    w = packed(codes, scales, zeros if given_zeros else None, group)
+    for got, want in zip(buffers(w), ref.linear_layout(codes, scales, zeros, group)):
+        assert np.array_equal(got, want)
+
+
+@pytest.mark.parametrize("rows,cols,group", [(5, 32, 32), (31, 192, 64), (64, 512, 128)])
+def test_quantization(rows, cols, group):
+    rng = np.random.default_rng(rows)
+    W = rng.standard_normal((rows, cols), dtype=np.float32) * 0.02
+    W[0, :group] = 0.0                       # a group of zeros: scale 1
+    W[1, :group] = np.abs(W[1, :group])      # one sign only
+    W[2, :group] = -np.abs(W[2, :group])
+    W[3, 3] = 1e30                           # the scale overflows: 1
+    w = api.linear_pack(torch.from_numpy(W).to(DEV), api.Linear.empty(rows, cols, group, DEV))
+    want = ref.linear_quantize(W, group)
+    for got, exp in zip(buffers(w), ref.linear_layout(*want, group)):
+        assert np.array_equal(got, exp)
+
+
+def check(T, rows, cols, group, x_dtype, y_dtype, bias, seed=0, shift=0.0):
+    rng = np.random.default_rng(seed)
+    codes, scales, zeros = weights(rows, cols, group, seed)
+    w = packed(codes, scales, zeros, group)
+    x = ref.as_type(rng.standard_normal((T, cols)) + shift, x_dtype)
+    b = rng.standard_normal(rows).astype(np.float32) if bias else None
+    guard = torch.full((T + 2, rows), -77.0, dtype=y_dtype, device=DEV)
+    y = api.linear_forward(x.to(DEV), w, None if b is None else torch.from_numpy(b).to(DEV),
+                           y=guard[1:T + 1])
+    want, err = ref.linear(ref.f64(x), codes, scales, zeros, group, b)
+    ref.close(y, want, err, y_dtype, (T, rows, cols, group))
+    assert (guard[0] == -77).all() and (guard[T + 1] == -77).all()
+
+
+@pytest.mark.parametrize("T", [1, 2, 15, 16, 17, 32, 33, 64, 65, 130])
+@pytest.mark.parametrize("x_dtype", [BF, F32])
+def test_tokens(T, x_dtype):
+    check(T, 48, 384, 128, x_dtype, x_dtype, bias=T % 2 == 0, seed=T)
+
+
+@pytest.mark.parametrize("rows", [1, 15, 16, 17, 100, 1003])
+@pytest.mark.parametrize("cols,group", [(32, 32), (96, 32), (64, 64), (192, 64), (1984, 64),
+                                        (128, 128), (1152, 128), (4096, 128)])
+def test_shapes(rows, cols, group):
+    check(3, rows, cols, group, BF, F32, bias=True, seed=rows + cols)
+    check(19, rows, cols, group, F32, BF, bias=False, seed=rows + cols)
+
+
+def test_activations_with_a_large_mean():
+    check(16, 64, 512, 128, BF, BF, bias=False, shift=30.0)
+    check(16, 64, 512, 128, F32, F32, bias=False, shift=30.0)
+
+
+def test_small_and_large_activations():
+    """Binary32 activations over the exponents that a product can have."""
+    codes, scales, zeros = weights(20, 256, 128)
+    w = packed(codes, scales, zeros, 128)
+    rng = np.random.default_rng(1)
+    x = (rng.standard_normal((6, 256)) * 10.0 ** np.array([-25, -10, 0, 5, 15, 30])[:, None]
+         ).astype(np.float32)
+    y = api.linear_forward(torch.from_numpy(x).to(DEV), w)
+    ref.close(y, *ref.linear(x.astype(np.float64), codes, scales, zeros, 128), F32)
+
+
+@pytest.mark.parametrize("x_dtype", [BF, F32])
+@pytest.mark.parametrize("value", [float("nan"), float("inf"), float("-inf")])
+def test_a_token_that_is_not_finite_stays_alone(x_dtype, value):
+    codes, scales, zeros = weights(20, 192, 64)
+    w = packed(codes, scales, zeros, 64)
+    x = torch.randn((18, 192), generator=torch.Generator().manual_seed(0)).to(x_dtype)
+    clean = api.linear_forward(x.to(DEV), w)
+    x[17, 100] = value
+    y = api.linear_forward(x.to(DEV), w)
+    assert torch.equal(y[:17], clean[:17])
+    assert not torch.isfinite(y[17]).any()
+
+
+def test_no_tokens():
+    w = packed(*weights(20, 64, 64), 64)
+    assert api.linear_forward(torch.empty((0, 64), device=DEV), w).shape == (0, 20)
+
+
+def test_rejects_wrong_arguments():
+    w = packed(*weights(20, 64, 64), 64)
+    x = torch.zeros((2, 64), device=DEV)
+    for bad in (x[:, :32], x.t().contiguous().t(), x.cpu()):
+        with pytest.raises(ValueError):
+            api.linear_forward(bad, w)
+    with pytest.raises(TypeError):
+        api.linear_forward(x.half(), w)
+    with pytest.raises(ValueError):
+        api.linear_forward(x, w, bias=torch.zeros(19, device=DEV))
+    with pytest.raises(ValueError):
+        api.linear_forward(x, w, y=torch.zeros((2, 19), device=DEV))
+    odd = torch.zeros(2 * 64 + 1, device=DEV)[1:].view(2, 64)      # not 16-byte aligned
+    with pytest.raises(api.D2MoEError) as e:
+        api.linear_forward(odd, w)
+    assert e.value.status == api.EINVAL
+
+
+def test_results_do_not_change_between_calls_and_streams():
+    codes, scales, zeros = weights(300, 1024, 128)
+    w = packed(codes, scales, zeros, 128)
+    x = torch.randn((40, 1024), device=DEV, dtype=BF)
+    torch.cuda.synchronize()
+    a = api.linear_forward(x, w)
+    s = torch.cuda.Stream()
+    b = api.linear_forward(x, w, stream=s)
+    c = api.linear_forward(x[:7].contiguous(), w)
+    torch.cuda.synchronize()
+    assert torch.equal(a, b)
+    assert torch.equal(a[:7], c)       # a token's result does not go by the batch
