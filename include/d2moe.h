@@ -437,14 +437,14 @@ d2moe_status d2moe_moe_forward_streamed(
  * A linear layer's weights in 4 bits with group scales: row r, column c is
  *     W[r][c] = scale[r][c / group] * (code[r][c] - zero[r][c / group]),
  * codes and zero points in 0..15.  group is 32, 64 or 128, cols % group == 0,
- * rows >= 1.  Stored in blocks of 16 rows by 128 columns, RB = ceil(rows/16)
- * block rows of KB = ceil(cols/128) blocks; what lies past the last row or
- * column is zero (codes, scales and zeros):
+ * cols <= 2^22, rows >= 1.  Stored in blocks of 16 rows by 128 columns, RB =
+ * ceil(rows/16) block rows of KB = ceil(cols/128) blocks; past the last row or
+ * column, codes, scales and zero points are 0:
  *   codes  [RB][KB][64][4] uint32: word j of lane l holds row 16 rb + l % 16,
  *          columns 128 kb + 32 j + 8 (l / 16) + e, e = 0..7, with code e at
  *          bits 4 (e / 2 + 4 (e % 2)) .. + 3;
  *   scales [RB][KB][128/group][16] binary16;
- *   zeros  [RB][KB][128/group][16] uint8.
+ *   zeros  [RB][KB][128/group][16] uint8, 16 + the zero point.
  * All three are device buffers of the sizes reported by d2moe_linear_size,
  * 16-byte aligned.
  */

@@ -5,20 +5,21 @@
 //
 // A code n becomes the bf16 number 16 + n by placing its four bits below the
 // leading one of 16 (0x4180): one shift and one and-or for two codes, exact.
-// The product with the 16 + z that has to be taken off again uses the sum of
-// x over the group, which a second MFMA with a matrix of ones leaves in the
-// same lanes as the first one's results.  16 rather than a larger power of two
-// keeps the two parts near the result's size (31 / 15 at most in the weights),
-// so the difference costs about one bit of binary32.
+// 16 + z times the sum of x over the group is taken off again.  16 rather than a
+// larger power of two keeps the two parts near the result's size (31 / 15 at
+// most in the weights), so the difference costs about one bit of binary32.
 //
 // bf16 activations are used as they are; binary32 ones as the sum of three
 // bf16 pieces of 8 bits each, which is exact.
+#include <type_traits>
+
 #include "decoder.h"
 
 namespace d2moe {
 namespace {
 
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 b2 __attribute__((ext_vector_type(2)));
 typedef float f4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u4 __attribute__((ext_vector_type(4)));
 
@@ -29,7 +30,7 @@ struct LinArgs {
   const uint8_t* zeros;
   const float* bias;
   void* y;
-  int T, rows, cols, KB;
+  int T, rows, cols, RB, KB;
   bool y_bf;
 };
 
@@ -39,141 +40,367 @@ struct LinArgs {
 __device__ inline f4 mma(u4 a, u4 b, f4 c) {
   f4 d = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a),
                                                  __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
-  asm("" : "+v"(d) : "v"(a), "v"(b), "v"(c));
+  asm("" : "+v"(d) : "v"(a), "v"(b));
   return d;
 }
 
-// The eight codes of a word as 16 + n in bf16 (pair p: codes 2 p, 2 p + 1).
-__device__ inline u4 decode(uint32_t w) {
-  constexpr uint32_t kMask = 0x00780078u, kOne = 0x41804180u;
-  return u4{((w << 3) & kMask) | kOne, ((w >> 1) & kMask) | kOne, ((w >> 5) & kMask) | kOne,
-            ((w >> 9) & kMask) | kOne};
+// The eight codes of a word as 16 + n in bf16 (pair p: codes 2 p, 2 p + 1), a
+// shift and an and-or each.  The instruction takes one constant from outside
+// the vector registers, so the mask is held in one.
+__device__ inline uint32_t code_mask() {
+  uint32_t m = 0x00780078u;
+  asm("" : "+v"(m));
+  return m;
+}
+__device__ inline u4 decode(uint32_t w, uint32_t mask) {
+  constexpr uint32_t kOne = 0x41804180u;
+  return u4{((w << 3) & mask) | kOne, ((w >> 1) & mask) | kOne, ((w >> 5) & mask) | kOne,
+            ((w >> 9) & mask) | kOne};
 }
 
-// The operand(s) of eight activations: NP = 1 for bf16, 3 pieces for binary32,
-// smallest first.  A piece is the value cut to its upper 16 bits, what is left
-// goes to the next; nothing is left of an infinity or NaN.
-template <int NP>
-struct XFrag {
-  u4 p[NP];
+// Eight activations as loaded; the operand(s) they become (NP = 1 for bf16, 3
+// pieces for binary32, smallest first) and their sum.  A piece is the value cut
+// to its upper 16 bits, what is left goes to the next (an infinity leaves NaN).
+template <typename TX>
+struct XRaw;
+template <>
+struct XRaw<uint16_t> {
+  static constexpr int NP = 1;
+  u4 v;
+  __device__ void load(const uint16_t* x) { v = *(const u4*)x; }
+  __device__ void pieces(u4 (&p)[1]) const { p[0] = v; }
+  __device__ float sum() const {
+    const b2 one = {(__bf16)1.0f, (__bf16)1.0f};
+    float s = 0.0f;
+#pragma unroll
+    for (int d = 0; d < 4; ++d)
+      s = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(b2, (uint32_t)v[d]), one, s, false);
+    return s;
+  }
 };
-__device__ inline XFrag<1> load_x(const uint16_t* x) { return {*(const u4*)x}; }
-__device__ inline XFrag<3> load_x(const float* x) {
-  const f4 a = *(const f4*)x, b = *(const f4*)(x + 4);
-  XFrag<3> f;
-  uint32_t h[3][8];
-#pragma unroll
-  for (int e = 0; e < 8; ++e) {
-    float v = e < 4 ? a[e & 3] : b[e & 3];
-    const bool finite = (__float_as_uint(v) & 0x7f800000u) != 0x7f800000u;
-#pragma unroll
-    for (int k = 2; k >= 0; --k) {
-      h[k][e] = __float_as_uint(v) & 0xffff0000u;
-      v -= __uint_as_float(h[k][e]);
-      v = finite ? v : 0.0f;
-    }
+template <>
+struct XRaw<float> {
+  static constexpr int NP = 3;
+  f4 v[2];
+  __device__ void load(const float* x) {
+    v[0] = *(const f4*)x;
+    v[1] = *(const f4*)(x + 4);
   }
+  __device__ void pieces(u4 (&p)[3]) const {
+    uint32_t h[3][8];
 #pragma unroll
-  for (int k = 0; k < 3; ++k)
+    for (int e = 0; e < 8; ++e) {
+      float f = v[e >> 2][e & 3];
 #pragma unroll
-    for (int d = 0; d < 4; ++d) f.p[k][d] = h[k][2 * d + 1] | h[k][2 * d] >> 16;
-  return f;
+      for (int k = 2; k >= 0; --k) {
+        h[k][e] = __float_as_uint(f);
+        f -= __uint_as_float(h[k][e] & 0xffff0000u);
+      }
+    }
+#pragma unroll
+    for (int k = 0; k < 3; ++k)
+#pragma unroll
+      for (int d = 0; d < 4; ++d)
+        p[k][d] = __builtin_amdgcn_perm(h[k][2 * d + 1], h[k][2 * d], 0x07060302u);
+  }
+  __device__ float sum() const {
+    const f4 s = v[0] + v[1];
+    return (s[0] + s[1]) + (s[2] + s[3]);
+  }
+};
+
+template <int CTRL>
+__device__ inline float dpp_add(float v) {
+  return v + __int_as_float(
+                 __builtin_amdgcn_update_dpp(0, __float_as_int(v), CTRL, 0xf, 0xf, true));
 }
 
-// A workgroup computes 16 rows by 16 NT tokens; its WAVES waves take column
-// blocks in turn and add up through LDS.  GB groups per block of 128 columns.
-template <typename TX, int NT, int GB, int WAVES>
-__global__ __launch_bounds__(64 * WAVES) void linear_kernel(LinArgs a) {
-  constexpr int NP = sizeof(TX) == 2 ? 1 : 3;
-  __shared__ f4 part[WAVES][NT][64];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, q = lane >> 4;
-  const int rb = blockIdx.x, t0 = blockIdx.y * 16 * NT;
-  const TX* xr[NT];
+// A barrier for LDS alone: a full one would also wait for the loads under way.
+__device__ inline void lds_barrier() {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
+  __builtin_amdgcn_s_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
+}
+
+// What a lane needs of one column block for RT row tiles, beside x.
+template <int RT, int GB>
+struct WFrag {
+  u4 w[RT];
+  uint2 s[RT][GB];     // four binary16 scales, rows 4 q .. 4 q + 3
+  uint32_t z[RT][GB];  // 16 + their zero points
+};
+template <int RT, int GB>
+__device__ inline void load_w(WFrag<RT, GB>& f, const LinArgs& a, int rb0, int kb, int lane) {
+  const uint32_t q = lane >> 4;
 #pragma unroll
-  for (int n = 0; n < NT; ++n) {
-    // tokens past the end repeat the last one; their results are not written
-    const int t = t0 + 16 * n + (lane & 15);
-    xr[n] = (const TX*)a.x + (int64_t)(t < a.T ? t : a.T - 1) * a.cols + 8 * q;
-  }
-  const u4 ones = {0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u};
-  f4 y[NT];
-#pragma unroll
-  for (int n = 0; n < NT; ++n) y[n] = f4{0.0f, 0.0f, 0.0f, 0.0f};
-  for (int kb = wave; kb < a.KB; kb += WAVES) {
-    const size_t blk = (size_t)rb * a.KB + kb;
-    const u4 w = *(const u4*)(a.codes + (blk * 64 + lane) * 4);
-    const uint16_t* sp = a.scales + blk * GB * kLinRows + 4 * q;
-    const uint8_t* zp = a.zeros + blk * GB * kLinRows + 4 * q;
-    const int c0 = kb * kLinCols;
+  for (int r = 0; r < RT; ++r) {
+    // row tiles past the end repeat the last one (their results are not
+    // written), and so do column blocks (their scales are taken as zero)
+    const int rb = rb0 + r < a.RB ? rb0 + r : a.RB - 1;
+    const size_t blk = (size_t)rb * a.KB + (kb < a.KB ? kb : a.KB - 1);
+    f.w[r] = *(const u4*)((const char*)a.codes + blk * 1024 + 16u * lane);
+    const char* sp = (const char*)a.scales + blk * (GB * kLinRows * 2);
+    const char* zp = (const char*)a.zeros + blk * (GB * kLinRows);
 #pragma unroll
     for (int g = 0; g < GB; ++g) {
-      const uint2 sw = *(const uint2*)(sp + g * kLinRows);
-      const uint32_t zw = *(const uint32_t*)(zp + g * kLinRows);
-      f4 acc[NT], xs[NT];
+      f.s[r][g] = *(const uint2*)(sp + (8u * q + g * kLinRows * 2));
+      f.z[r][g] = *(const uint32_t*)(zp + (4u * q + g * kLinRows));
+    }
+  }
+}
+
+// A workgroup computes 16 RT R rows by 16 NT tokens: R waves side by side in the
+// rows times S that take column blocks in turn and add up through LDS.  GB
+// groups per block of 128 columns.
+//
+// The activations of a column block go through LDS, for the R waves that share
+// them and because rows of them are whole cache lines while an operand is 16
+// pieces of 64 bytes, which the L1 takes twice as long for.  The 16-byte piece of
+// token t, columns 8 c .. 8 c + 7 of the block, lies where lane (c % 4, t % 16 ^ c)
+// of operand c / 4 reads it: 16 neighbouring lanes meet 16 different bank groups
+// writing (one token) and reading (one c).  The group sums of x are taken on the
+// way.
+//
+// Weights and activations are loaded two steps before their use.
+template <typename TX, int NT, int NU, int RT, int R, int S, int GB>
+__global__ __launch_bounds__(64 * R * S) void linear_kernel(LinArgs a) {
+  constexpr int NP = XRaw<TX>::NP, kUnits = (NU + R - 1) / R;
+  // the first pieces of binary32 activations are summed apart from the rest:
+  // their products have 13 bits, so that sum is nearly exact, and what the
+  // 16 + z cancels of it is not rounded at the size of the uncancelled sum
+  constexpr int NA = NP == 1 ? 1 : 2;
+  struct Stage {
+    u4 x[2][S][NP][NT * 4 * 64];
+    float sum[2][S][GB][NT * 16];
+  };
+  union Lds {
+    Stage st;
+    f4 part[S][R * RT][NT][64];
+  };
+  __shared__ Lds lds;
+  const int lane = threadIdx.x & 63, q = lane >> 4, col = lane & 15;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);  // addresses stay scalar
+  const int rw = wave % R, sk = wave / R;
+  const int rb0 = (blockIdx.x * R + rw) * RT, t0 = blockIdx.y * 16 * NT;
+  const int steps = (a.KB + S - 1) / S;
+
+  // NU units of 4 tokens by 128 columns (fewer than 4 NT where there are no more
+  // tokens); a lane has 8 columns of one token.  Tokens past the last repeat it
+  // (their results are not written), and so do columns and blocks (their scales
+  // are taken as zero): every load is made, so that a wait can count on those
+  // behind the one it is for.
+  uint32_t xrow[kUnits];
 #pragma unroll
-      for (int n = 0; n < NT; ++n) acc[n] = xs[n] = f4{0.0f, 0.0f, 0.0f, 0.0f};
+  for (int i = 0; i < kUnits; ++i) {
+    const int t = 4 * (rw + R * i) + q;
+    xrow[i] = (uint32_t)(t < a.T - t0 ? t : a.T - t0 - 1) * a.cols;
+  }
+  auto load_x = [&](XRaw<TX> (&x)[kUnits], int kb) {
+    const int c0 = (kb < a.KB ? kb : a.KB - 1) * kLinCols;
+    const char* xk = (const char*)a.x + ((int64_t)t0 * a.cols + c0) * sizeof(TX);
+    int c = 8 * col;
+    if constexpr (GB > 1) c = c < a.cols - c0 ? c : a.cols - c0 - 8;
+#pragma unroll
+    for (int i = 0; i < kUnits; ++i) x[i].load((const TX*)(xk + (xrow[i] + c) * (uint32_t)sizeof(TX)));
+  };
+  auto store_x = [&](const XRaw<TX> (&x)[kUnits], int buf) {
+#pragma unroll
+    for (int i = 0; i < kUnits; ++i) {
+      const int unit = rw + R * i;
+      if (NU % R != 0 && unit >= NU) break;
+      const int t = 4 * unit + q;
+      u4 p[NP];
+      x[i].pieces(p);
+#pragma unroll
+      for (int k = 0; k < NP; ++k)
+        lds.st.x[buf][sk][k][((t >> 4) * 4 + (col >> 2)) * 64 + (col & 3) * 16 +
+                             ((t & 15) ^ col)] = p[k];
+      float s = x[i].sum();
+      s = dpp_add<0xB1>(s);                        // quads: lane ^ 1, lane ^ 2
+      s = dpp_add<0x4E>(s);
+      if constexpr (GB <= 2) s = dpp_add<0x141>(s);  // halves of a row of 16, mirrored
+      if constexpr (GB == 1) s = dpp_add<0x140>(s);  // the row, mirrored
+      if (col % (16 / GB) == 0) lds.st.sum[buf][sk][col / (16 / GB)][t] = s;
+    }
+  };
+  // a step's activations are shared by R waves, or stay within one
+  auto hand_over = [&] {
+    if constexpr (R > 1) {
+      lds_barrier();
+    } else {
+      __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+      __builtin_amdgcn_wave_barrier();
+      __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+    }
+  };
+
+  const uint32_t mask = code_mask();
+  const f4 zero = {0.0f, 0.0f, 0.0f, 0.0f};
+  float y[RT][NT][4];
+#pragma unroll
+  for (int r = 0; r < RT; ++r)
+#pragma unroll
+    for (int n = 0; n < NT; ++n)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) y[r][n][i] = 0.0f;
+  // Step `it` with its weights; x holds the activations of the next step.  Both
+  // are loaded again, for two steps on, as soon as they have been used.
+  auto step = [&](int it, auto parity, WFrag<RT, GB>& w, XRaw<TX> (&x)[kUnits]) {
+    constexpr int buf = decltype(parity)::value;
+    const bool live = it * S + sk < a.KB;  // a block past the last one adds nothing
+    // operands of the activations, read one word ahead of their products
+    u4 xp[2][NT][NP];
+    auto read_x = [&](int j) {
+#pragma unroll
+      for (int n = 0; n < NT; ++n)
+#pragma unroll
+        for (int k = 0; k < NP; ++k)
+          xp[j & 1][n][k] = lds.st.x[buf][sk][k][(n * 4 + j) * 64 + q * 16 + (col ^ (4 * j + q))];
+    };
+    read_x(0);
+#pragma unroll
+    for (int g = 0; g < GB; ++g) {
+      f4 acc[RT][NT][NA];
+#pragma unroll
+      for (int n = 0; n < NT; ++n)
+#pragma unroll
+        for (int h = 0; h < NA; ++h)
+#pragma unroll
+          for (int r = 0; r < RT; ++r) acc[r][n][h] = zero;
+      float xs[NT];
+#pragma unroll
+      for (int n = 0; n < NT; ++n) xs[n] = lds.st.sum[buf][sk][g][16 * n + col];
 #pragma unroll
       for (int jj = 0; jj < 4 / GB; ++jj) {
         const int j = g * (4 / GB) + jj;
-        // past the last column (cols is a multiple of 32) the scale is zero
-        // and any columns of the same token do
-        const int c = GB > 1 && c0 + 32 * j >= a.cols ? c0 : c0 + 32 * j;
-        const u4 wa = decode(w[j]);
+        if (j < 3) read_x(j + 1);
+        __builtin_amdgcn_sched_barrier(0);
+        u4 wa[RT];
 #pragma unroll
-        for (int n = 0; n < NT; ++n) {
-          const XFrag<NP> xf = load_x(xr[n] + c);
+        for (int r = 0; r < RT; ++r) wa[r] = decode(w.w[r][j], mask);
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
 #pragma unroll
           for (int k = 0; k < NP; ++k) {
-            acc[n] = mma(wa, xf.p[k], acc[n]);
-            xs[n] = mma(ones, xf.p[k], xs[n]);
+            const int h = k == NP - 1 ? 0 : 1;
+#pragma unroll
+            for (int r = 0; r < RT; ++r) acc[r][n][h] = mma(wa[r], xp[j & 1][n][k], acc[r][n][h]);
+          }
+      }
+#pragma unroll
+      for (int r = 0; r < RT; ++r) {
+        const uint2 sc = live ? w.s[r][g] : make_uint2(0, 0);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const float s = h2f((uint16_t)((i < 2 ? sc.x : sc.y) >> (16 * (i & 1))));
+          const float z = (float)((w.z[r][g] >> (8 * i)) & 255u);  // 16 + zero point
+#pragma unroll
+          for (int n = 0; n < NT; ++n) {
+            float v = fmaf(-z, xs[n], acc[r][n][0][i]);
+            if constexpr (NA == 2) v += acc[r][n][1][i];
+            y[r][n][i] = fmaf(s, v, y[r][n][i]);
           }
         }
       }
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const float s = h2f((uint16_t)((i < 2 ? sw.x : sw.y) >> (16 * (i & 1))));
-        const float z = 16.0f + (float)((zw >> (8 * i)) & 255u);
-#pragma unroll
-        for (int n = 0; n < NT; ++n) y[n][i] = fmaf(s, fmaf(-z, xs[n][i], acc[n][i]), y[n][i]);
-      }
     }
+    load_w(w, a, rb0, (it + 2) * S + sk, lane);
+    store_x(x, buf ^ 1);
+    load_x(x, (it + 3) * S + sk);
+    hand_over();
+  };
+  WFrag<RT, GB> w0, w1;
+  XRaw<TX> x0[kUnits], x1[kUnits];
+  load_x(x0, sk);
+  load_w(w0, a, rb0, sk, lane);
+  load_x(x1, S + sk);
+  load_w(w1, a, rb0, S + sk, lane);
+  store_x(x0, 0);
+  load_x(x0, 2 * S + sk);
+  hand_over();
+  for (int it = 0; it < steps; it += 2) {
+    step(it, std::integral_constant<int, 0>{}, w0, x1);
+    if (it + 1 == steps) break;
+    step(it + 1, std::integral_constant<int, 1>{}, w1, x0);
   }
+  lds_barrier();  // the buffers become the waves' results
 #pragma unroll
-  for (int n = 0; n < NT; ++n) part[wave][n][lane] = y[n];
-  __syncthreads();
-  // result r of token t lies in lane 16 (r / 4) + t % 16 of tile t / 16, row r % 4
-  for (int o = threadIdx.x; o < 256 * NT; o += 64 * WAVES) {
-    const int r = o & 15, t = o >> 4, row = rb * kLinRows + r;
+  for (int r = 0; r < RT; ++r)
+#pragma unroll
+    for (int n = 0; n < NT; ++n)
+      lds.part[sk][rw * RT + r][n][lane] = f4{y[r][n][0], y[r][n][1], y[r][n][2], y[r][n][3]};
+  lds_barrier();
+  // row 16 r + i of token 16 n + t lies in tile (r, n), lane 16 (i / 4) + t, i % 4
+  constexpr int kRows = 16 * R * RT;
+  for (int o = threadIdx.x; o < kRows * 16 * NT; o += 64 * R * S) {
+    const int i = o % kRows, t = o / kRows, row = blockIdx.x * kRows + i;
     if (row >= a.rows || t0 + t >= a.T) continue;
     float sum = 0.0f;
 #pragma unroll
-    for (int w = 0; w < WAVES; ++w) sum += part[w][t >> 4][(r >> 2) * 16 + (t & 15)][r & 3];
+    for (int w = 0; w < S; ++w)
+      sum += lds.part[w][i >> 4][t >> 4][((i & 15) >> 2) * 16 + (t & 15)][i & 3];
     if (a.bias) sum += a.bias[row];
-    const int64_t at = (int64_t)(t0 + t) * a.rows + row;
+    const int64_t to = (int64_t)(t0 + t) * a.rows + row;
     if (a.y_bf)
-      ((uint16_t*)a.y)[at] = f2bf(sum);
+      ((uint16_t*)a.y)[to] = f2bf(sum);
     else
-      ((float*)a.y)[at] = sum;
+      ((float*)a.y)[to] = sum;
   }
 }
 
-template <typename TX, int NT, int WAVES>
-hipError_t run_linear_g(const LinArgs& a, int group, hipStream_t s) {
-  const dim3 grid((a.rows - 1) / kLinRows + 1, (a.T - 1) / (16 * NT) + 1);
-  if (group == 128)
-    linear_kernel<TX, NT, 1, WAVES><<<grid, 64 * WAVES, 0, s>>>(a);
-  else if (group == 64)
-    linear_kernel<TX, NT, 2, WAVES><<<grid, 64 * WAVES, 0, s>>>(a);
-  else
-    linear_kernel<TX, NT, 4, WAVES><<<grid, 64 * WAVES, 0, s>>>(a);
+template <typename TX, int NT, int NU, int RT, int R, int S, int GB>
+hipError_t run_linear_g(const LinArgs& a, hipStream_t s) {
+  const dim3 grid((a.RB - 1) / (RT * R) + 1, (a.T - 1) / (16 * NT) + 1);
+  linear_kernel<TX, NT, NU, RT, R, S, GB><<<grid, 64 * R * S, 0, s>>>(a);
   return hipGetLastError();
 }
 
-template <typename TX>
-hipError_t run_linear(const LinArgs& a, int group, hipStream_t s) {
-  if (a.T <= 16) return run_linear_g<TX, 1, 8>(a, group, s);
-  if (a.T <= 32) return run_linear_g<TX, 2, 8>(a, group, s);
-  return run_linear_g<TX, 4, 8>(a, group, s);
+// The division of the work goes by the number of 16 x 16 tiles of the result.
+// Up to one per CU, a workgroup takes one tile and its waves divide the columns;
+// with more, workgroups of 2, 4 and 8 row tiles share the activations (whose
+// reading from L2 bounds the kernel otherwise) while one round of workgroups
+// still fills the chip.  Measured, bf16, 4096 columns, group 128, us (R, S):
+//   4096 rows x 16 (256 tiles):  1, 8: 6.1   2, 4: 7.3   4, 4: 8.7   8, 2: 12.5
+//   6144 rows x 16 (384 tiles):  1, 8: 8.9   2, 4: 7.6   4, 4: 8.8   8, 2: 12.6
+//   4096 rows x 64 (1024 tiles): 2, 4: 10.6  4, 4: 9.3   8, 2: 12.5
+//   32000 rows x 16:             4, 4: 18.1  8, 2: 16.7
+//   32000 rows x 64:             8, 2: 55.8; 32 tokens, 8, 2: 35.4; 64 tokens, RT 2, 4, 2: 30.2
+// Binary32 activations take three times the LDS and twice the time.
+constexpr int kCus = 256;
+
+template <int NU, int GB>
+hipError_t run_linear_16(const LinArgs& a, int64_t tiles, hipStream_t s) {
+  if (tiles <= kCus) {
+    // long rows at one to four tokens: 16 waves keep more loads under way (14336
+    // columns 9.0 us, with 8 waves 10.7; 4096 columns 4.5 and 4.4)
+    if constexpr (NU == 1)
+      if (a.KB > 48) return run_linear_g<uint16_t, 1, NU, 1, 1, 16, GB>(a, s);
+    return run_linear_g<uint16_t, 1, NU, 1, 1, 8, GB>(a, s);
+  }
+  if (tiles <= 2 * kCus) return run_linear_g<uint16_t, 1, NU, 1, 2, 4, GB>(a, s);
+  if (tiles <= 4 * kCus) return run_linear_g<uint16_t, 1, NU, 1, 4, 4, GB>(a, s);
+  return run_linear_g<uint16_t, 1, NU, 1, 8, 2, GB>(a, s);
+}
+template <int NU, int GB>
+hipError_t run_linear_32(const LinArgs& a, int64_t tiles, hipStream_t s) {
+  if constexpr (NU == 1)
+    if (tiles <= kCus) return run_linear_g<float, 1, NU, 1, 1, 6, GB>(a, s);
+  // groups of 32 need more registers than 16 waves have
+  if (tiles <= 2 * kCus || GB == 4) return run_linear_g<float, 1, NU, 1, 2, 4, GB>(a, s);
+  if constexpr (GB < 4) return run_linear_g<float, 1, NU, 1, 4, 4, GB>(a, s);
+}
+
+template <int GB>
+hipError_t run_linear(const LinArgs& a, bool x_bf, hipStream_t s) {
+  const int64_t tiles = (int64_t)a.RB * ((a.T + 15) / 16);
+  if constexpr (GB < 4)  // as above
+    if (tiles > 8 * kCus && a.T > 16) {
+      if (!x_bf) return run_linear_g<float, 2, 8, GB == 1 ? 2 : 1, 4, 2, GB>(a, s);
+      if (a.T <= 32) return run_linear_g<uint16_t, 2, 8, 1, 8, 2, GB>(a, s);
+      return run_linear_g<uint16_t, 4, 16, 2, 4, 2, GB>(a, s);
+    }
+  if (a.T <= 4) return x_bf ? run_linear_16<1, GB>(a, tiles, s) : run_linear_32<1, GB>(a, tiles, s);
+  if (a.T <= 8) return x_bf ? run_linear_16<2, GB>(a, tiles, s) : run_linear_32<2, GB>(a, tiles, s);
+  return x_bf ? run_linear_16<4, GB>(a, tiles, s) : run_linear_32<4, GB>(a, tiles, s);
 }
 
 }  // namespace
@@ -182,9 +409,11 @@ hipError_t launch_linear(const void* x, d2moe_dtype xd, int T, const d2moe_linea
                          const float* bias, void* y, d2moe_dtype yd, hipStream_t s) {
   if (T == 0) return hipSuccess;
   const LinArgs a{x, w->codes, w->scales, w->zeros, bias, y, T, w->rows, w->cols,
-                  lin_col_blocks(w), yd == D2MOE_BF16};
-  return xd == D2MOE_BF16 ? run_linear<uint16_t>(a, w->group, s)
-                          : run_linear<float>(a, w->group, s);
+                  lin_row_blocks(w), lin_col_blocks(w), yd == D2MOE_BF16};
+  const bool x_bf = xd == D2MOE_BF16;
+  return w->group == 128  ? run_linear<1>(a, x_bf, s)
+         : w->group == 64 ? run_linear<2>(a, x_bf, s)
+                          : run_linear<4>(a, x_bf, s);
 }
 
 }  // namespace d2moe

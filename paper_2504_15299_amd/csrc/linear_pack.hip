@@ -100,7 +100,7 @@ __global__ __launch_bounds__(64 * kPackWaves) void linear_pack_kernel(const floa
     if (q == 0 && j % per == 0) {
       const size_t at = (blk * gb + j / per) * kLinRows + r;
       o.scales[at] = s_h;
-      o.zeros[at] = (uint8_t)(int)z;
+      o.zeros[at] = (uint8_t)(16 + (int)z);
     }
   }
   *(uint4*)(o.codes + (blk * 64 + lane) * 4) = make_uint4(word[0], word[1], word[2], word[3]);
@@ -130,7 +130,7 @@ __global__ __launch_bounds__(64 * kPackWaves) void linear_pack_codes_kernel(
       const size_t at = (blk * gb + j / per) * kLinRows + r;
       const size_t from = (size_t)row * (o.cols / o.group) + c / o.group;
       o.scales[at] = inside ? scales[from] : (uint16_t)0;
-      o.zeros[at] = !inside ? (uint8_t)0 : zeros ? (uint8_t)(zeros[from] & 15) : (uint8_t)8;
+      o.zeros[at] = (uint8_t)(16 + (!inside ? 0 : zeros ? zeros[from] & 15 : 8));
     }
   }
   *(uint4*)(o.codes + (blk * 64 + lane) * 4) = make_uint4(word[0], word[1], word[2], word[3]);

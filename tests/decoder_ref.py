@@ -44,8 +44,8 @@ def linear_layout(codes, scales, zeros, group):
     full[:rows, :cols] = codes
     s = np.zeros((RB * 16, KB * GB), np.float16)
     s[:rows, :cols // group] = scales
-    z = np.zeros((RB * 16, KB * GB), np.uint8)
-    z[:rows, :cols // group] = zeros
+    z = np.full((RB * 16, KB * GB), 16, np.uint8)
+    z[:rows, :cols // group] += zeros
     words = np.zeros((RB, KB, 64, 4), np.uint32)
     for lane in range(64):
         for j in range(4):

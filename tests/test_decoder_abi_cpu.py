@@ -29,7 +29,7 @@ def linear(**kw):
 
 BAD_LINEARS = [dict(rows=0), dict(rows=-16), dict(cols=0), dict(cols=-256), dict(cols=200),
                dict(cols=32), dict(group=16), dict(group=0), dict(group=256), dict(codes=0),
-               dict(scales=0), dict(zeros=0), dict(codes=ODD), dict(cols=(1 << 24) + 64)]
+               dict(scales=0), dict(zeros=0), dict(codes=ODD), dict(cols=(1 << 22) + 64)]
 
 
 @pytest.mark.parametrize("rows,cols,group", [(1, 32, 32), (16, 128, 128), (17, 160, 32),
