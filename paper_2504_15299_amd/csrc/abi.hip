@@ -382,7 +382,8 @@ d2moe_status d2moe_kv_append(const void* q, int64_t q_stride, int32_t q_heads, c
 
 static bool attn_shape_ok(int B, int q_heads, int n_heads, int dim, int max_len) {
   return B >= 0 && B <= 65535 && n_heads >= 1 && q_heads >= n_heads && q_heads <= 65535 &&
-         q_heads % n_heads == 0 && dim >= 8 && dim <= 256 && dim % 8 == 0 && max_len >= 0;
+         q_heads % n_heads == 0 && dim >= 8 && dim <= 256 && dim % 8 == 0 && max_len >= 0 &&
+         (int64_t)B * q_heads <= (1 << 22);  // workgroups of a launch
 }
 
 d2moe_status d2moe_attn_decode_workspace(int32_t B, int32_t q_heads, int32_t n_heads,

@@ -12,8 +12,10 @@
 // keys that a lane computed, and V^T is read to match: no exchange between the
 // products, only the maximum crosses lanes.
 //
-// The keys are split over workgroups (and their waves); splits leave their m, l
-// and O in the workspace and a second kernel joins them.
+// The tiles of all sequences and key heads stand in one row that is cut into
+// equal shares, one a workgroup, so that sequences of any lengths fill the chip
+// evenly.  A share that holds a key head's tiles only in part leaves its m, l and
+// O in the workspace, and a second kernel joins the parts.
 //
 // Bound by reading the cache: 4 len head_dim bytes (bf16) per key head against
 // 16-column products that would take a twentieth of that time.
@@ -28,22 +30,24 @@ typedef float f2 __attribute__((ext_vector_type(2)));
 typedef float f4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u4 __attribute__((ext_vector_type(4)));
 
-constexpr int kAttnWaves = 4;
-constexpr int kAttnThreads = 64 * kAttnWaves;
 constexpr int kHeadTile = 16;    // query heads of a workgroup
 constexpr int kKeysAhead = 1024; // keys whose row offsets are held in LDS at a time
-constexpr int kSplitUnit = 128;  // keys of a split are a multiple of this
-constexpr int kSplitGroups = 2048;  // workgroups aimed at
+constexpr int kWholeKeys = 512;  // up to here a workgroup takes a unit whole,
+constexpr int kManyUnits = 96;   // up to twice as many with that many units
+constexpr int kMaxSplitUnits = 2048;
+constexpr int kSplitSeqs = 256;  // most sequences of a call whose keys are split
+constexpr int kMinShare = 4;     // tiles
+constexpr int kCus = 256;
 
 struct AttnArgs {
   const void *q, *k, *v;
   int64_t q_stride, page_stride, token_stride, head_stride;
   const int32_t *table, *lengths;
   FastDiv page;
-  int n_pages, max_pages, Hq, H, G, tiles, D, window, n_splits, chunk;
+  int B, n_pages, max_pages, Hq, H, G, tiles, D, window, groups;
   float scale_log2;  // scale / ln 2
   void* out;
-  float *part_o, *part_ml;  // [B][Hq][n_splits][D], [B][Hq][n_splits][2]
+  float *part_o, *part_ml;  // [groups][2][min(G, 16)] rows of D and of 2
 };
 
 // Keys of sequence b that are attended: [first, first + count).
@@ -53,6 +57,51 @@ __device__ inline void key_range(const AttnArgs& a, int b, int& first, int& coun
   n = n < 0 ? 0 : n > room ? (int)room : n;
   first = a.window > 0 && n > a.window ? n - a.window : 0;
   count = n - first;
+}
+
+// Where the tiles of each sequence stand in the row of all: sequence b's units
+// (key heads times head tiles, `per` of them) one after the other, t_b tiles each,
+// from per * (t_0 + .. + t_{b-1}) on.  Held by every wave in its registers, lane
+// l the sequences 4 l .. 4 l + 3.  (The host sees to it that the row has fewer
+// than 2^31 tiles.)
+struct Row {
+  int upto[4];  // tiles of the sequences up to and with this one, one unit each
+  int total;
+};
+__device__ inline Row row_of_tiles(const AttnArgs& a, int tk) {
+  const int lane = threadIdx.x & 63;
+  Row r;
+  int sum = 0;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    int first, count = 0;
+    if (4 * lane + i < a.B) key_range(a, 4 * lane + i, first, count);
+    sum += (count + tk - 1) / tk;
+    r.upto[i] = sum;
+  }
+  int inc = sum;  // over the lanes: within rows of 16, then across the rows
+  inc += __builtin_amdgcn_update_dpp(0, inc, 0x111, 0xf, 0xf, true);
+  inc += __builtin_amdgcn_update_dpp(0, inc, 0x112, 0xf, 0xf, true);
+  inc += __builtin_amdgcn_update_dpp(0, inc, 0x114, 0xf, 0xf, true);
+  inc += __builtin_amdgcn_update_dpp(0, inc, 0x118, 0xf, 0xf, true);
+  const int r0 = __builtin_amdgcn_readlane(inc, 15), r1 = __builtin_amdgcn_readlane(inc, 31),
+            r2 = __builtin_amdgcn_readlane(inc, 47);
+  inc += lane < 16 ? 0 : lane < 32 ? r0 : lane < 48 ? r0 + r1 : r0 + r1 + r2;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) r.upto[i] += inc - sum;
+  r.total = __builtin_amdgcn_readlane(inc, 63);
+  return r;
+}
+__device__ inline int row_upto(const Row& r, int b) {  // uniform; 0 for b = -1
+  if (b < 0) return 0;
+  const int i = b & 3;
+  return __builtin_amdgcn_readlane(
+      i == 0 ? r.upto[0] : i == 1 ? r.upto[1] : i == 2 ? r.upto[2] : r.upto[3], b >> 2);
+}
+// Tiles of a share: the row in equal parts, but kMinShare at least.
+__device__ inline int row_share(const Row& r, int per, int groups) {
+  const int share = (int)(((int64_t)r.total * per + groups - 1) / groups);
+  return share > kMinShare ? share : kMinShare;
 }
 
 __device__ inline float fast_exp2(float x) { return __builtin_amdgcn_exp2f(x); }
@@ -227,11 +276,16 @@ struct Tile<float, DP, PAD> {
         for (int e = 0; e < 4; ++e) o.f[j][h][e] = at[j] < 0 ? 0.0f : o.f[j][h][e];
   }
   __device__ static void scores(float (&s)[NV], const K& k, const Q& q) {
-    f4 acc = {0.0f, 0.0f, 0.0f, 0.0f};
+    f4 acc = mma(k.f[0][0], q.f[0][0], f4{0.0f, 0.0f, 0.0f, 0.0f});
 #pragma unroll
     for (int c = 0; c < KS; ++c)
 #pragma unroll
-      for (int e = 0; e < 4; ++e) acc = mma(k.f[c][e], q.f[c][e], acc);
+      for (int e = 0; e < 4; ++e) {
+        if (c == 0 && e == 0) continue;
+        f4 sum = mma(k.f[c][e], q.f[c][e], acc);
+        asm("" : "+v"(sum) : "v"(acc));  // nor shares part of them with the sum so far
+        acc = sum;
+      }
 #pragma unroll
     for (int i = 0; i < 4; ++i) s[i] = acc[i];
   }
@@ -245,73 +299,129 @@ struct Tile<float, DP, PAD> {
   }
 };
 
-template <typename T, int DP, bool PAD>
-__global__ __launch_bounds__(kAttnThreads, 1) void attn_decode_kernel(AttnArgs a) {
+// A barrier for LDS alone: a full one would also wait for the loads under way.
+__device__ inline void lds_barrier() {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
+  __builtin_amdgcn_s_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
+}
+
+// Four values of a result row.
+template <typename T>
+__device__ inline void store4(T* p, f4 v) {
+  if constexpr (sizeof(T) == 2)
+    *(uint2*)p = make_uint2(f2bf(v[0]) | (uint32_t)f2bf(v[1]) << 16,
+                            f2bf(v[2]) | (uint32_t)f2bf(v[3]) << 16);
+  else
+    *(f4*)p = v;
+}
+
+// WAVES waves take tiles of TK keys in turn; HT: query heads that the workgroup
+// may have (4 or 16; columns past them are computed on zeros).  SPLIT: a
+// workgroup takes its share of the row of tiles, otherwise one unit whole.
+//
+// The row offsets of up to kKeysAhead keys are worked out by all threads into
+// LDS (-1: masked), so that no lookup in the block table stands between the
+// loads of the loop.  The next tile's keys are loaded while this one's values
+// are used.  Every load of the loop is made, on whatever row where there is no
+// key: a wait can then count on the loads behind the one it is for.
+template <typename T, int DP, bool PAD, int HT, int WAVES, bool SPLIT>
+__global__ __launch_bounds__(64 * WAVES, DP <= 128 ? 2 : 1) void attn_decode_kernel(AttnArgs a) {
   using M = Tile<T, DP, PAD>;
-  constexpr int kPitch = DP + 4;
-  __shared__ int64_t off[kKeysAhead];
-  __shared__ float sm[kAttnWaves][kHeadTile], sl[kAttnWaves][kHeadTile];
-  __shared__ __align__(16) float so[kAttnWaves][kHeadTile][kPitch];
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, col = lane & 15, q = lane >> 4;
-  const int b = blockIdx.y;
-  int unit = blockIdx.x;
-  const int split = unit % a.n_splits;
-  unit /= a.n_splits;
-  const int hk = unit % a.H, tile = unit / a.H;
-  int first, count;
-  key_range(a, b, first, count);
-  if (a.n_splits > 1 && (int64_t)split * a.chunk >= count) return;
-  const int g0 = tile * kHeadTile;                               // of the key head's G heads
-  const int heads = a.G - g0 < kHeadTile ? a.G - g0 : kHeadTile;  // of this workgroup
-  const int h0 = hk * a.G + g0;
-  const T* kc = (const T*)a.k + hk * a.head_stride;
-  const T* vc = (const T*)a.v + hk * a.head_stride;
+  struct Join {
+    float m[WAVES][HT], l[WAVES][HT];
+    __align__(16) float o[WAVES][HT][DP + 4];
+  };
+  union Lds {
+    int64_t off[kKeysAhead];
+    Join join;
+  };
+  __shared__ Lds lds;
+  const int tid = threadIdx.x, lane = tid & 63, col = lane & 15, q = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int per = a.H * a.tiles;  // units of a sequence
 
-  typename M::Q qf;
-  M::load_q(qf, (const T*)a.q + b * a.q_stride + (int64_t)(h0 + (col < heads ? col : 0)) * a.D, q,
-            a.D, col < heads);
-  float m = -INFINITY, l = 0.0f;
-  f4 o[M::H][M::VE];
+  // tiles at .. end - 1 of the row, or the one unit
+  Row row;
+  int at = blockIdx.x, end = blockIdx.x + 1;
+  if constexpr (SPLIT) {
+    row = row_of_tiles(a, M::TK);
+    const int share = row_share(row, per, a.groups);
+    const int64_t to = ((int64_t)blockIdx.x + 1) * share, all = (int64_t)row.total * per;
+    if (to - share >= all) return;
+    at = (int)(to - share);
+    end = (int)(to < all ? to : all);
+  }
+  while (at < end) {
+    // the next segment: tiles j0 .. j1 - 1 of unit `unit` of sequence b
+    int b, unit, j0 = 0, j1, seq_tiles, first, count;
+    if constexpr (SPLIT) {
+      b = 0;
 #pragma unroll
-  for (int h = 0; h < M::H; ++h)
+      for (int i = 0; i < 4; ++i) b += __popcll(__ballot(row.upto[i] * per <= at));
+      const int before = row_upto(row, b - 1);
+      seq_tiles = row_upto(row, b) - before;
+      const uint32_t in = at - before * per;
+      unit = in / (uint32_t)seq_tiles;
+      j0 = in - unit * seq_tiles;
+      j1 = seq_tiles - j0 < end - at ? seq_tiles : j0 + (end - at);
+      key_range(a, b, first, count);
+    } else {
+      b = at / per;
+      unit = at - b * per;
+      key_range(a, b, first, count);
+      j1 = seq_tiles = (count + M::TK - 1) / M::TK;
+    }
+    const int hk = unit % a.H, tile = unit / a.H;
+    const int g0 = tile * kHeadTile;                               // of the key head's G heads
+    const int heads = a.G - g0 < kHeadTile ? a.G - g0 : kHeadTile;  // of this unit
+    const int h0 = hk * a.G + g0;
+    const T* kc = (const T*)a.k + hk * a.head_stride;
+    const T* vc = (const T*)a.v + hk * a.head_stride;
+    typename M::Q qf;
+    M::load_q(qf, (const T*)a.q + b * a.q_stride + (int64_t)(h0 + (col < heads ? col : 0)) * a.D,
+              q, a.D, col < heads);
+    float m = -INFINITY, l = 0.0f;
+    f4 o[M::H][M::VE];
 #pragma unroll
-    for (int i = 0; i < M::VE; ++i) o[h][i] = f4{0.0f, 0.0f, 0.0f, 0.0f};
+    for (int h = 0; h < M::H; ++h)
+#pragma unroll
+      for (int i = 0; i < M::VE; ++i) o[h][i] = f4{0.0f, 0.0f, 0.0f, 0.0f};
 
-  // chunks split, split + n_splits, ... of the sequence's keys
-  for (int64_t c0 = (int64_t)split * a.chunk; c0 < count; c0 += (int64_t)a.n_splits * a.chunk) {
-    const int c1 = c0 + a.chunk < count ? (int)c0 + a.chunk : count;
-    for (int s0 = (int)c0; s0 < c1; s0 += kKeysAhead) {
-      const int n = c1 - s0 < kKeysAhead ? c1 - s0 : kKeysAhead;
-      const int nt = (n + M::TK - 1) / M::TK;
-      __syncthreads();  // the offsets before these have been used
-      for (int i = tid; i < nt * M::TK; i += kAttnThreads) {
-        int64_t at = -1;
-        if (i < n) {
+    constexpr int kTilesAhead = kKeysAhead / M::TK;
+    for (int t0 = j0; t0 < j1; t0 += kTilesAhead) {
+      const int nt = j1 - t0 < kTilesAhead ? j1 - t0 : kTilesAhead;
+      const int s0 = t0 * M::TK;
+      lds_barrier();  // what was there has been used
+      for (int i = tid; i < nt * M::TK; i += 64 * WAVES) {
+        int64_t to = -1;
+        if (s0 + i < count) {
           const uint32_t key = (uint32_t)(first + s0 + i), c = a.page.div(key);
           const int page = a.table[(int64_t)b * a.max_pages + c];
           if ((uint32_t)page < (uint32_t)a.n_pages)
-            at = page * a.page_stride + (int64_t)(key - c * a.page.d) * a.token_stride;
+            to = page * a.page_stride + (int64_t)(key - c * a.page.d) * a.token_stride;
         }
-        off[i] = at;
+        lds.off[i] = to;
       }
-      __syncthreads();
+      lds_barrier();
+      if (wave >= nt) continue;  // no barrier until the next offsets
       typename M::K kf;
-      if (wave < nt) M::load_k(kf, kc, off + wave * M::TK, lane, a.D);
-      for (int t = wave; t < nt; t += kAttnWaves) {
-        int64_t at[M::NV];
+      M::load_k(kf, kc, lds.off + wave * M::TK, lane, a.D);
+      for (int t = wave; t < nt; t += WAVES) {
+        int64_t from[M::NV];
 #pragma unroll
-        for (int j = 0; j < M::NV; ++j) at[j] = off[t * M::TK + M::key_of(j, q)];
+        for (int j = 0; j < M::NV; ++j) from[j] = lds.off[t * M::TK + M::key_of(j, q)];
         typename M::V vf;
-        M::load_v(vf, vc, at, lane, a.D);
+        M::load_v(vf, vc, from, lane, a.D);
         float s[M::NV];
         M::scores(s, kf, qf);
-        if (t + kAttnWaves < nt) M::load_k(kf, kc, off + (t + kAttnWaves) * M::TK, lane, a.D);
+        M::load_k(kf, kc, lds.off + (t + WAVES < nt ? t + WAVES : t) * M::TK, lane, a.D);
         bool hole = false;
         float mx = -INFINITY;
 #pragma unroll
         for (int j = 0; j < M::NV; ++j) {
-          s[j] = at[j] < 0 ? -INFINITY : s[j] * a.scale_log2;
-          hole |= at[j] < 0;
+          s[j] = from[j] < 0 ? -INFINITY : s[j] * a.scale_log2;
+          hole |= from[j] < 0;
           mx = fmaxf(mx, s[j]);
         }
         mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
@@ -332,131 +442,199 @@ __global__ __launch_bounds__(kAttnThreads, 1) void attn_decode_kernel(AttnArgs a
 #pragma unroll
             for (int i = 0; i < M::VE; ++i) o[h][i] *= alpha;
         }
-        if (__any(hole)) M::clear_v(vf, at);  // 0 times what a masked row holds is not 0
+        if (__any(hole)) M::clear_v(vf, from);  // 0 times what a masked row holds is not 0
         M::values(o, s, vf);
       }
     }
-  }
 
-  // join the waves: every head's m, l and O
-  l += __shfl_xor(l, 16, 64);
-  l += __shfl_xor(l, 32, 64);
-  if (q == 0) {
-    sm[wave][col] = m;
-    sl[wave][col] = l;
-  }
-#pragma unroll
-  for (int h = 0; h < M::H; ++h)
-#pragma unroll
-    for (int r = 0; r < 4; ++r)
-#pragma unroll
-      for (int i = 0; i < M::VE; i += 4)
-        *(f4*)&so[wave][col][16 * M::VE * h + M::VE * (4 * q + r) + i] =
-            f4{o[h][i][r], o[h][i + 1][r], o[h][i + 2][r], o[h][i + 3][r]};
-  __syncthreads();
-  const int per = a.D / 4;
-  for (int i = tid; i < heads * per; i += kAttnThreads) {
-    const int g = i / per, d = (i - g * per) * 4;
-    float mm = -INFINITY;
-#pragma unroll
-    for (int w = 0; w < kAttnWaves; ++w) mm = fmaxf(mm, sm[w][g]);
-    const float ref = mm == -INFINITY ? 0.0f : mm;
-    float ll = 0.0f;
-    f4 acc = {0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-    for (int w = 0; w < kAttnWaves; ++w) {
-      const float f = fast_exp2(sm[w][g] - ref);
-      ll = fmaf(f, sl[w][g], ll);
-      acc += f * *(const f4*)&so[w][g][d];
-    }
-    const int64_t row = (int64_t)b * a.Hq + h0 + g;
-    if (a.n_splits > 1) {
-      *(f4*)(a.part_o + (row * a.n_splits + split) * a.D + d) = acc;
-      if (d == 0) {
-        a.part_ml[(row * a.n_splits + split) * 2] = mm;
-        a.part_ml[(row * a.n_splits + split) * 2 + 1] = ll;
+    // join the waves: every head's m, l and O
+    lds_barrier();  // the offsets have been used
+    l += __shfl_xor(l, 16, 64);
+    l += __shfl_xor(l, 32, 64);
+    if (col < HT) {
+      if (q == 0) {
+        lds.join.m[wave][col] = m;
+        lds.join.l[wave][col] = l;
       }
-      continue;
+#pragma unroll
+      for (int h = 0; h < M::H; ++h)
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+#pragma unroll
+          for (int i = 0; i < M::VE; i += 4)
+            *(f4*)&lds.join.o[wave][col][16 * M::VE * h + M::VE * (4 * q + r) + i] =
+                f4{o[h][i][r], o[h][i + 1][r], o[h][i + 2][r], o[h][i + 3][r]};
     }
-    acc *= ll == 0.0f ? 0.0f : 1.0f / ll;
-    if constexpr (sizeof(T) == 2)
-      *(uint2*)((uint16_t*)a.out + row * a.D + d) =
-          make_uint2(f2bf(acc[0]) | (uint32_t)f2bf(acc[1]) << 16,
-                     f2bf(acc[2]) | (uint32_t)f2bf(acc[3]) << 16);
-    else
-      *(f4*)((float*)a.out + row * a.D + d) = acc;
+    lds_barrier();
+    const int row4 = a.D / 4;
+    for (int i = tid; i < heads * row4; i += 64 * WAVES) {
+      const int g = i / row4, d = (i - g * row4) * 4;
+      float mm = -INFINITY;
+#pragma unroll
+      for (int w = 0; w < WAVES; ++w) mm = fmaxf(mm, lds.join.m[w][g]);
+      const float ref = mm == -INFINITY ? 0.0f : mm;
+      float ll = 0.0f;
+      f4 acc = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+      for (int w = 0; w < WAVES; ++w) {
+        const float f = fast_exp2(lds.join.m[w][g] - ref);
+        ll = fmaf(f, lds.join.l[w][g], ll);
+        acc += f * *(const f4*)&lds.join.o[w][g][d];
+      }
+      if (SPLIT && j1 - j0 < seq_tiles) {
+        // a share has one part at most that begins a unit and one that does not
+        const int rows = a.G < kHeadTile ? a.G : kHeadTile;
+        const int64_t to = ((int64_t)blockIdx.x * 2 + (j0 > 0 ? 0 : 1)) * rows + g;
+        *(f4*)(a.part_o + to * a.D + d) = acc;
+        if (d == 0) *(float2*)(a.part_ml + to * 2) = make_float2(mm, ll);
+      } else {
+        store4((T*)a.out + ((int64_t)b * a.Hq + h0 + g) * a.D + d,
+               acc * (ll == 0.0f ? 0.0f : 1.0f / ll));
+      }
+    }
+    if constexpr (SPLIT) at += j1 - j0;
+    else at = end;
   }
 }
 
-// Joins the splits of one query head, four values a thread.
-template <typename T>
-__global__ __launch_bounds__(64) void attn_join_kernel(AttnArgs a) {
-  const int64_t row = (int64_t)blockIdx.y * a.Hq + blockIdx.x;
-  const int d = threadIdx.x * 4;
-  if (d >= a.D) return;
-  int first, count;
-  key_range(a, blockIdx.y, first, count);
-  const int used = (int)(((int64_t)count + a.chunk - 1) / a.chunk);
-  const int n = used < a.n_splits ? used : a.n_splits;
-  const float* ml = a.part_ml + row * a.n_splits * 2;
-  float mm = -INFINITY;
-  for (int i = 0; i < n; ++i) mm = fmaxf(mm, ml[2 * i]);
-  const float ref = mm == -INFINITY ? 0.0f : mm;
-  float ll = 0.0f;
+// Joins the parts of one query head: the waves (a lane has four values) take
+// parts in turn.  A unit that one share holds whole is done already, one without
+// keys gives zeros.
+constexpr int kJoinWaves = 4;
+template <typename T, int TK>
+__global__ __launch_bounds__(64 * kJoinWaves) void attn_join_kernel(AttnArgs a) {
+  __shared__ float pm[kJoinWaves], pl[kJoinWaves];
+  __shared__ __align__(16) f4 po[kJoinWaves][64];
+  const int b = blockIdx.y, head = blockIdx.x;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int per = a.H * a.tiles, rows = a.G < kHeadTile ? a.G : kHeadTile;
+  const int hk = head / a.G, tile = (head - hk * a.G) / kHeadTile;
+  const int g = head - hk * a.G - tile * kHeadTile;
+  const Row row = row_of_tiles(a, TK);
+  const int share = row_share(row, per, a.groups);
+  const int before = row_upto(row, b - 1), tiles = row_upto(row, b) - before;
+  const int from = before * per + (tile * a.H + hk) * tiles;
+  const int w0 = from / share, n = tiles == 0 ? 0 : (from + tiles - 1) / share - w0 + 1;
+  if (n == 1) return;
+  const int d = 4 * lane < a.D ? 4 * lane : 0;
+  // part i lies in share w0 + i; the first begins the unit
+  auto part = [&](int i) { return ((int64_t)(w0 + i) * 2 + (i == 0 ? 1 : 0)) * rows + g; };
+  float mm = -INFINITY, ll = 0.0f;
   f4 acc = {0.0f, 0.0f, 0.0f, 0.0f};
-  for (int i = 0; i < n; ++i) {
-    const float f = fast_exp2(ml[2 * i] - ref);
-    ll = fmaf(f, ml[2 * i + 1], ll);
-    acc += f * *(const f4*)(a.part_o + (row * a.n_splits + i) * a.D + d);
+  constexpr int kAhead = 4;  // parts loaded together
+  for (int i = wave; i < n; i += kAhead * kJoinWaves) {
+    float2 ml[kAhead];
+    f4 v[kAhead];
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k) {
+      const int64_t p = part(i + k * kJoinWaves < n ? i + k * kJoinWaves : i);
+      ml[k] = *(const float2*)(a.part_ml + p * 2);
+      v[k] = *(const f4*)(a.part_o + p * a.D + d);
+    }
+    float top = mm;
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k) top = fmaxf(top, ml[k].x);
+    const float ref = top == -INFINITY ? 0.0f : top, alpha = fast_exp2(mm - ref);
+    mm = top;
+    ll *= alpha;
+    acc *= alpha;
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k) {
+      if (i + k * kJoinWaves >= n) break;
+      const float f = fast_exp2(ml[k].x - ref);
+      ll = fmaf(f, ml[k].y, ll);
+      acc += f * v[k];
+    }
   }
-  acc *= ll == 0.0f ? 0.0f : 1.0f / ll;
-  if constexpr (sizeof(T) == 2)
-    *(uint2*)((uint16_t*)a.out + row * a.D + d) =
-        make_uint2(f2bf(acc[0]) | (uint32_t)f2bf(acc[1]) << 16,
-                   f2bf(acc[2]) | (uint32_t)f2bf(acc[3]) << 16);
-  else
-    *(f4*)((float*)a.out + row * a.D + d) = acc;
+  po[wave][lane] = acc;
+  if (lane == 0) pm[wave] = mm, pl[wave] = ll;
+  __syncthreads();
+  if (wave != 0 || 4 * lane >= a.D) return;
+#pragma unroll
+  for (int w = 1; w < kJoinWaves; ++w) mm = fmaxf(mm, pm[w]);
+  const float ref = mm == -INFINITY ? 0.0f : mm;
+  ll = 0.0f;
+  acc = f4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+  for (int w = 0; w < kJoinWaves; ++w) {
+    const float f = fast_exp2(pm[w] - ref);
+    ll = fmaf(f, pl[w], ll);
+    acc += f * po[w][lane];
+  }
+  store4((T*)a.out + ((int64_t)b * a.Hq + head) * a.D + d,
+         acc * (ll == 0.0f ? 0.0f : 1.0f / ll));
 }
 
 int head_tiles(int q_heads, int n_heads) {
   return (q_heads / n_heads + kHeadTile - 1) / kHeadTile;
 }
 
-// Most splits that a call with lengths up to max_len makes: enough workgroups
-// to fill the chip, but kSplitUnit keys each at least.  Grows with max_len.
-int most_splits(int B, int q_heads, int n_heads, int max_len) {
-  const int64_t units = (int64_t)B * n_heads * head_tiles(q_heads, n_heads);
-  const int64_t want = units == 0 ? 1 : (kSplitGroups + units - 1) / units;
-  const int64_t fit = ((int64_t)max_len + kSplitUnit - 1) / kSplitUnit;
-  const int64_t n = want < fit ? want : fit;
-  return n < 1 ? 1 : (int)n;
+int head_units(int B, int q_heads, int n_heads) {
+  return B * n_heads * head_tiles(q_heads, n_heads);  // at most 65535 * 65535 / 2, checked first
+}
+
+// Workgroups of a call whose keys are split: one per CU, whose four waves keep
+// enough loads under way (64 sequences of 8192 keys, 8 heads of 128: 371 us; with
+// two 386); two where the units are many and short, so that one's start and end
+// lie under the other's loads (32 sequences of up to 2000 keys, 40 heads: 144
+// and 133 us), or the rows short (16 heads of 64: 21.6 and 20.0 us).
+int split_groups(int units, int dim) {
+  return kCus * (dim <= 64 || (dim <= 128 && units > 512) ? 2 : 1);
+}
+
+// Whether the keys are split.  Not where a second kernel and the look over all
+// lengths cost more than the split saves: few keys, or whole units that fill the
+// chip (64 sequences of up to 1000 keys, 8 heads of 128: whole 38.8 us, split
+// 45.0; up to 2000 keys 74 and 65 us; 4 sequences of 1000 keys 15.1 and 12.5
+// us).  Nor where a row of tiles could pass 2^31.
+bool attn_splits(int B, int q_heads, int n_heads, int keys, int64_t room) {
+  if (B > kSplitSeqs) return false;
+  const int64_t units = head_units(B, q_heads, n_heads);
+  return keys > (units < kManyUnits ? kWholeKeys : 2 * kWholeKeys) && units < kMaxSplitUnits &&
+         units * ((room < 0x7fffffff ? room : 0x7fffffff) / 16 + 1) < 0x7fffffff;
+}
+
+template <typename T, int DP, bool PAD, int HT>
+void run_attn_h(const AttnArgs& a, bool split, hipStream_t s) {
+  const int units = a.B * a.H * a.tiles;
+  if (split)
+    attn_decode_kernel<T, DP, PAD, HT, 4, true><<<a.groups, 256, 0, s>>>(a);
+  else if (DP <= 128 && units <= kCus)  // more waves a unit, where the chip has room
+    attn_decode_kernel<T, DP, PAD, HT, DP <= 128 ? 8 : 4, false><<<units, 512, 0, s>>>(a);
+  else
+    attn_decode_kernel<T, DP, PAD, HT, 4, false><<<units, 256, 0, s>>>(a);
 }
 
 template <typename T, int DP, bool PAD>
-void run_attn(const AttnArgs& a, dim3 grid, hipStream_t s) {
-  attn_decode_kernel<T, DP, PAD><<<grid, kAttnThreads, 0, s>>>(a);
+hipError_t run_attn(const AttnArgs& a, bool split, hipStream_t s) {
+  if (a.G <= 4)
+    run_attn_h<T, DP, PAD, 4>(a, split, s);
+  else
+    run_attn_h<T, DP, PAD, 16>(a, split, s);
+  const hipError_t err = hipGetLastError();
+  if (err != hipSuccess || !split) return err;
+  attn_join_kernel<T, Tile<T, DP, PAD>::TK>
+      <<<dim3(a.Hq, a.B), 64 * kJoinWaves, 0, s>>>(a);
+  return hipGetLastError();
 }
 
 template <typename T>
-hipError_t run_attn_t(const AttnArgs& a, int B, hipStream_t s) {
-  const dim3 grid(a.n_splits * a.H * a.tiles, B);
-  if (a.D == 64) run_attn<T, 64, false>(a, grid, s);
-  else if (a.D < 64) run_attn<T, 64, true>(a, grid, s);
-  else if (a.D == 128) run_attn<T, 128, false>(a, grid, s);
-  else if (a.D < 128) run_attn<T, 128, true>(a, grid, s);
-  else if (a.D == 256) run_attn<T, 256, false>(a, grid, s);
-  else run_attn<T, 256, true>(a, grid, s);
-  hipError_t err = hipGetLastError();
-  if (err != hipSuccess || a.n_splits == 1) return err;
-  attn_join_kernel<T><<<dim3(a.Hq, B), 64, 0, s>>>(a);
-  return hipGetLastError();
+hipError_t run_attn_t(const AttnArgs& a, bool split, hipStream_t s) {
+  if (a.D == 64) return run_attn<T, 64, false>(a, split, s);
+  if (a.D < 64) return run_attn<T, 64, true>(a, split, s);
+  if (a.D == 128) return run_attn<T, 128, false>(a, split, s);
+  if (a.D < 128) return run_attn<T, 128, true>(a, split, s);
+  if (a.D == 256) return run_attn<T, 256, false>(a, split, s);
+  return run_attn<T, 256, true>(a, split, s);
 }
 
 }  // namespace
 
 size_t attn_decode_workspace(int B, int q_heads, int n_heads, int dim, int max_len) {
-  const int n = most_splits(B, q_heads, n_heads, max_len);
-  return n == 1 ? 0 : (size_t)B * q_heads * n * (dim + 2) * sizeof(float);
+  if (B == 0 || !attn_splits(B, q_heads, n_heads, max_len, 0)) return 0;
+  const int rows = q_heads / n_heads < kHeadTile ? q_heads / n_heads : kHeadTile;
+  return (size_t)split_groups(head_units(B, q_heads, n_heads), dim) * 2 * rows * (dim + 2) *
+         sizeof(float);
 }
 
 hipError_t launch_attn_decode(const void* q, int64_t q_stride, int B, int q_heads,
@@ -468,19 +646,20 @@ hipError_t launch_attn_decode(const void* q, int64_t q_stride, int B, int q_head
   a.q = q, a.k = c->k, a.v = c->v, a.q_stride = q_stride, a.page_stride = c->page_stride;
   a.token_stride = c->token_stride, a.head_stride = c->head_stride;
   a.table = table, a.lengths = lengths, a.page = fast_div(c->page_size);
-  a.n_pages = c->n_pages, a.max_pages = max_pages, a.Hq = q_heads, a.H = c->n_heads;
+  a.B = B, a.n_pages = c->n_pages, a.max_pages = max_pages, a.Hq = q_heads, a.H = c->n_heads;
   a.G = q_heads / c->n_heads, a.tiles = head_tiles(q_heads, c->n_heads), a.D = c->head_dim;
   a.window = window;
   const int keys = window > 0 && window < max_len ? window : max_len;
-  const int n = most_splits(B, q_heads, c->n_heads, keys);
-  const int units = (int)(((int64_t)keys + n - 1) / n + kSplitUnit - 1) / kSplitUnit;
-  a.chunk = (units < 1 ? 1 : units) * kSplitUnit;
-  a.n_splits = keys > 0 ? (int)(((int64_t)keys + a.chunk - 1) / a.chunk) : 1;
+  const bool split =
+      attn_splits(B, q_heads, c->n_heads, keys, (int64_t)max_pages * c->page_size);
+  a.groups = split_groups(head_units(B, q_heads, c->n_heads), a.D);
   a.scale_log2 = scale * 1.44269504088896340736f;
   a.out = out;
+  const int rows = a.G < kHeadTile ? a.G : kHeadTile;
   a.part_o = (float*)ws;
-  a.part_ml = (float*)ws + (size_t)B * q_heads * a.n_splits * a.D;
-  return c->dtype == D2MOE_BF16 ? run_attn_t<uint16_t>(a, B, s) : run_attn_t<float>(a, B, s);
+  a.part_ml = (float*)ws + (size_t)a.groups * 2 * rows * a.D;
+  return c->dtype == D2MOE_BF16 ? run_attn_t<uint16_t>(a, split, s)
+                                : run_attn_t<float>(a, split, s);
 }
 
 }  // namespace d2moe

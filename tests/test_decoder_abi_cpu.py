@@ -106,7 +106,8 @@ def test_attn_decode_refusals():
     refuses("d2moe_attn_decode", ok, [dict(c=cache(**b)) for b in BAD_CACHES])
     refuses("d2moe_attn_decode", ok, [
         dict(q=None), dict(o=None), dict(ln=None), dict(bt=None), dict(q=ODD), dict(o=ODD),
-        dict(qs=504), dict(qs=516), dict(B=-1), dict(B=65536), dict(h=0), dict(h=6), dict(h=3),
+        dict(qs=504), dict(qs=516), dict(B=-1), dict(B=65536),
+        dict(B=65535, h=128, qs=8192), dict(h=0), dict(h=6), dict(h=3),
         dict(h=65536), dict(mp=-1), dict(ml=-1), dict(w=-1), dict(sc=float("nan")),
         dict(sc=float("inf"))])
     refuses("d2moe_attn_decode", ok, [dict(ws=None), dict(ws=ODD), dict(n=16)], api.EWORKSPACE)
@@ -123,7 +124,7 @@ def test_attn_decode_workspace():
         return n.value
 
     assert need(1, 8, 8, 64, 0) == need(1, 8, 8, 64, 128) == need(0, 8, 8, 64, 10 ** 6) == 0
-    assert need(4096, 32, 8, 128, 10 ** 6) == 0
+    assert need(4096, 32, 8, 128, 10 ** 6) == 0 < need(64, 32, 8, 128, 4096)
     last = 0
     for length in range(0, 40000, 37):
         assert need(2, 8, 2, 64, length) >= last

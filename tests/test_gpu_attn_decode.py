@@ -91,6 +91,28 @@ def test_long_and_the_length_expected(max_len, dtype):
     check(*make([2600, 1025, 1, 0], 2, 1, 64, 16, dtype), max_len=max_len)
 
 
+# the work in equal shares over all sequences, or whole per key head: batches of
+# empty, short and long sequences, more of them than a wave has lanes and than a
+# split call may have, key heads with more than 16 query heads
+@pytest.mark.parametrize("B,Hq,H,D", [(2, 8, 8, 64), (70, 4, 2, 64), (256, 2, 1, 16),
+                                      (257, 2, 1, 16), (30, 20, 1, 136), (5, 34, 2, 128)])
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("max_len", [100, 4000])
+def test_shares(B, Hq, H, D, dtype, max_len):
+    rng = np.random.default_rng(B)
+    lengths = rng.integers(0, 60, B)
+    lengths[rng.random(B) < 0.3] = 0
+    lengths[rng.integers(0, B, max(1, B // 20))] = rng.integers(300, 700)
+    check(*make(lengths.tolist(), Hq, H, D, 16, dtype, seed=B), max_len=max_len)
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+def test_all_empty(dtype):
+    for max_len in (10, 5000):
+        out = check(*make([0, 0, 0], 4, 2, 64, 16, dtype), max_len=max_len)
+        assert (out == 0).all()
+
+
 @pytest.mark.parametrize("window", [1, 2, 16, 31, 100, 128, 299, 300, 301, 5000])
 @pytest.mark.parametrize("dtype", [BF, F32])
 def test_window(window, dtype):
