@@ -419,40 +419,40 @@ def residual_rmsnorm(x: torch.Tensor, y: torch.Tensor | None, eps: float = 1e-5,
 
 # ---- the rest of a decoder block: 4-bit linear layers, paged cache, norms ------
 
-def _f32(t, shape, dev, what, dtype=torch.float32):
-    """Pointer of an optional contiguous tensor of this shape and type."""
-    if t is None:
-        return None
-    if t.dtype != dtype or tuple(t.shape) != shape or t.device != dev or not t.is_contiguous():
+def _arg(t, shape, dtype, dev, what):
+    """Pointer of a contiguous tensor of this shape and type."""
+    if t.dtype != dtype or t.shape != shape or t.device != dev or not t.is_contiguous():
         raise ValueError(f"{what} must be a contiguous {dtype} tensor of shape {shape} on {dev}")
     return t.data_ptr()
 
 
-def _i32(t, shape, dev, what):
-    return _f32(t, shape, dev, what, torch.int32)
-
-
-def _new(shape, dtype, dev, stream):
+def _new(like, shape, dtype, stream):
     """A tensor for a call on ``stream`` (None: the current one)."""
-    t = torch.empty(shape, dtype=dtype, device=dev)
+    t = like.new_empty(shape, dtype=dtype)
     if stream is not None:
         t.record_stream(stream)
     return t
 
 
+_CODES = {torch.float32: D2MOE_F32, torch.bfloat16: D2MOE_BF16}
+_entry = {}     # entry points by name
+
+
 def _run(name, dev, stream, *args):
     """The entry point on ``stream`` (None: the current one of the tensors'
     device), with that device current."""
-    if dev.type != "cuda":
+    fn = _entry.get(name)
+    if fn is None:
+        fn = _entry[name] = getattr(lib(), name)
+    index = dev.index
+    if dev.type != "cuda" or index is None:
         raise ValueError(f"{name}: tensors must be on a GPU, not on {dev}")
-    if stream is None:
-        stream = torch.cuda.current_stream(dev)
-    fn = getattr(lib(), name)
-    if dev.index == torch.cuda.current_device():
-        rc = fn(*args, stream.cuda_stream)
+    raw = torch._C._cuda_getCurrentRawStream(index) if stream is None else stream.cuda_stream
+    if index == torch._C._cuda_getDevice():
+        rc = fn(*args, raw)
     else:
-        with torch.cuda.device(dev):
-            rc = fn(*args, stream.cuda_stream)
+        with torch.cuda.device(index):
+            rc = fn(*args, raw)
     if rc != OK:
         raise D2MoEError(name, rc)
 
@@ -477,6 +477,7 @@ class Linear:
         self.codes, self.scales, self.zeros = codes, scales, zeros
         self._c = _Linear(rows, cols, group, codes.data_ptr(), scales.data_ptr(),
                           zeros.data_ptr())
+        self._ref = ctypes.byref(self._c)
 
     @staticmethod
     def empty(rows, cols, group=128, device="cuda"):
@@ -492,8 +493,8 @@ class Linear:
 def linear_pack(W: torch.Tensor, out: Linear, stream=None) -> Linear:
     """``d2moe_linear_pack``: quantize + pack W [rows][cols] (fp32, device)."""
     dev = out.codes.device
-    _run("d2moe_linear_pack", dev, stream, _f32(W, (out.rows, out.cols), dev, "W"), D2MOE_F32,
-         ctypes.byref(out._c))
+    _run("d2moe_linear_pack", dev, stream,
+         _arg(W, (out.rows, out.cols), torch.float32, dev, "W"), D2MOE_F32, out._ref)
     return out
 
 
@@ -503,9 +504,9 @@ def linear_pack_codes(codes: torch.Tensor, scales: torch.Tensor, zeros, out: Lin
     [rows][cols/group] float16, zeros [rows][cols/group] uint8 or None (8)."""
     dev, g = out.codes.device, (out.rows, out.cols // out.group)
     _run("d2moe_linear_pack_codes", dev, stream,
-         _f32(codes, (out.rows, out.cols), dev, "codes", torch.uint8),
-         _f32(scales, g, dev, "scales", torch.float16), _f32(zeros, g, dev, "zeros", torch.uint8),
-         ctypes.byref(out._c))
+         _arg(codes, (out.rows, out.cols), torch.uint8, dev, "codes"),
+         _arg(scales, g, torch.float16, dev, "scales"),
+         None if zeros is None else _arg(zeros, g, torch.uint8, dev, "zeros"), out._ref)
     return out
 
 
@@ -513,13 +514,18 @@ def linear_forward(x: torch.Tensor, w: Linear, bias: torch.Tensor | None = None,
                    y: torch.Tensor | None = None, y_dtype=None, stream=None) -> torch.Tensor:
     """``d2moe_linear_forward``: x [T][cols] -> [T][rows] (y_dtype, x's type
     when not given); bias [rows] float32 or None."""
-    T, dev = x.shape[0], w.codes.device
-    px = _f32(x, (T, w.cols), dev, "x", x.dtype)
+    T, dev, dtype = x.shape[0], w.codes.device, x.dtype
+    px = _arg(x, (T, w.cols), dtype, dev, "x")
     if y is None:
-        y = _new((T, w.rows), x.dtype if y_dtype is None else y_dtype, dev, stream)
-    _run("d2moe_linear_forward", dev, stream, px, _dtype_code(x), T, ctypes.byref(w._c),
-         _f32(bias, (w.rows,), dev, "bias"), _f32(y, (T, w.rows), dev, "y", y.dtype),
-         _dtype_code(y))
+        y = _new(x, (T, w.rows), y_dtype or dtype, stream)
+        py = y.data_ptr()
+    else:
+        py = _arg(y, (T, w.rows), y.dtype, dev, "y")
+    if dtype not in _CODES or y.dtype not in _CODES:
+        raise TypeError(f"unsupported dtypes {dtype}, {y.dtype}")
+    _run("d2moe_linear_forward", dev, stream, px, _CODES[dtype], T, w._ref,
+         None if bias is None else _arg(bias, (w.rows,), torch.float32, dev, "bias"), py,
+         _CODES[y.dtype])
     return y
 
 
@@ -536,6 +542,7 @@ class KVCache:
         self.k, self.v = k, v
         self.n_pages, self.page_size, self.n_heads, self.head_dim = k.shape
         self._c = _KVCache(*k.shape, _dtype_code(k), *k.stride()[:3], k.data_ptr(), v.data_ptr())
+        self._ref = ctypes.byref(self._c)
 
     @staticmethod
     def empty(n_pages, page_size, n_heads, head_dim, dtype=torch.bfloat16, device="cuda"):
@@ -544,13 +551,16 @@ class KVCache:
                        torch.empty(shape, dtype=dtype, device=device))
 
 
-def _rows(t, heads, dim, dev, what):
+def _rows(t, shape, dtype, dev, what):
     """Pointer and token stride of a [token][head][dim] tensor whose heads are
     packed."""
-    if t.dim() != 3 or tuple(t.shape[1:]) != (heads, dim) or t.device != dev or \
-            t.stride(2) != 1 or (heads > 1 and t.stride(1) != dim):
-        raise ValueError(f"{what} must be a [token][{heads}][{dim}] tensor on {dev}, heads packed")
-    return t.data_ptr(), t.stride(0) if t.shape[0] > 1 else heads * dim
+    if t.shape != shape or t.dtype != dtype or t.device != dev:
+        raise ValueError(f"{what} must be a {dtype} tensor of shape {shape} on {dev}")
+    n, heads, dim = shape
+    row, head, one = t.stride()
+    if one != 1 or (heads > 1 and head != dim):
+        raise ValueError(f"{what} must have its heads packed")
+    return t.data_ptr(), row if n > 1 else heads * dim
 
 
 def kv_append(q, k: torch.Tensor, v: torch.Tensor, cache: KVCache, block_table: torch.Tensor,
@@ -561,26 +571,32 @@ def kv_append(q, k: torch.Tensor, v: torch.Tensor, cache: KVCache, block_table: 
     [n_seqs][max_pages], positions [N] and token_seq [N] int32, cos and sin
     [n_rot][dim/2] float32.  Returns q_out [N][q_heads][dim] of the cache's
     type (None without q)."""
-    dev, N, D = cache.k.device, k.shape[0], cache.head_dim
-    pk, ks = _rows(k, cache.n_heads, D, dev, "k")
-    pv, vs = _rows(v, cache.n_heads, D, dev, "v")
-    if v.shape[0] != N or v.dtype != k.dtype or (N > 1 and vs != ks):
-        raise ValueError("v must match k")
+    dev, dtype, N, D = cache.k.device, k.dtype, k.shape[0], cache.head_dim
+    shape = (N, cache.n_heads, D)
+    pk, ks = _rows(k, shape, dtype, dev, "k")
+    pv, vs = _rows(v, shape, dtype, dev, "v")
+    if vs != ks:
+        raise ValueError("k and v must have the same token stride")
+    if dtype not in _CODES:
+        raise TypeError(f"unsupported dtype {dtype}")
     pq, qs, heads, po = None, 0, 0, None
     if q is not None:
         heads = q.shape[1]
-        pq, qs = _rows(q, heads, D, dev, "q")
-        if q.shape[0] != N or q.dtype != k.dtype:
-            raise ValueError("q must match k")
+        pq, qs = _rows(q, (N, heads, D), dtype, dev, "q")
         if q_out is None:
-            q_out = _new((N, heads, D), cache.k.dtype, dev, stream)
-        po = _f32(q_out, (N, heads, D), dev, "q_out", cache.k.dtype)
+            q_out = _new(k, (N, heads, D), cache.k.dtype, stream)
+            po = q_out.data_ptr()
+        else:
+            po = _arg(q_out, (N, heads, D), cache.k.dtype, dev, "q_out")
     n_seqs, pages = block_table.shape
+    i32, f32 = torch.int32, torch.float32
     n_rot = 0 if cos is None else cos.shape[0]
-    _run("d2moe_kv_append", dev, stream, pq, qs, heads, pk, pv, ks, _dtype_code(k), N,
-         ctypes.byref(cache._c), _i32(block_table, (n_seqs, pages), dev, "block_table"), n_seqs,
-         pages, _i32(positions, (N,), dev, "positions"), _i32(token_seq, (N,), dev, "token_seq"),
-         _f32(cos, (n_rot, D // 2), dev, "cos"), _f32(sin, (n_rot, D // 2), dev, "sin"), n_rot, po)
+    _run("d2moe_kv_append", dev, stream, pq, qs, heads, pk, pv, ks, _CODES[dtype], N, cache._ref,
+         _arg(block_table, (n_seqs, pages), i32, dev, "block_table"), n_seqs, pages,
+         _arg(positions, (N,), i32, dev, "positions"),
+         None if token_seq is None else _arg(token_seq, (N,), i32, dev, "token_seq"),
+         None if cos is None else _arg(cos, (n_rot, D // 2), f32, dev, "cos"),
+         None if sin is None else _arg(sin, (n_rot, D // 2), f32, dev, "sin"), n_rot, po)
     return q_out
 
 
@@ -600,27 +616,29 @@ def attn_decode(q: torch.Tensor, cache: KVCache, block_table: torch.Tensor, leng
     block_table [B][max_pages] and lengths [B] int32 (device) -> out
     [B][q_heads][dim].  ``scale`` is 1 / sqrt(dim) when not given, ``max_len``
     the length that fills a row of the table."""
-    dev, D = cache.k.device, cache.head_dim
-    if q.dim() != 3 or q.dtype != cache.k.dtype:
-        raise ValueError(f"q must be a [B][q_heads][{D}] tensor of the cache's type")
+    dev, dtype, D = cache.k.device, cache.k.dtype, cache.head_dim
     B, heads = q.shape[:2]
-    pq, qs = _rows(q, heads, D, dev, "q")
+    shape = (B, heads, D)
+    pq, qs = _rows(q, shape, dtype, dev, "q")
     pages = block_table.shape[1]
     if max_len is None:
         max_len = min(pages * cache.page_size, 0x7fffffff)
     if out is None:
-        out = _new((B, heads, D), q.dtype, dev, stream)
+        out = _new(q, shape, dtype, stream)
+        po = out.data_ptr()
+    else:
+        po = _arg(out, shape, dtype, dev, "out")
     if workspace is None:
         need = attn_decode_workspace(B, heads, cache, max_len)
-        workspace = _new((need,), torch.uint8, dev, stream) if need else None
+        if need:
+            workspace = _new(q, (need,), torch.uint8, stream)
     elif workspace.device != dev or not workspace.is_contiguous():
         raise ValueError(f"workspace must be a contiguous tensor on {dev}")
-    _run("d2moe_attn_decode", dev, stream, pq, qs, B, heads, ctypes.byref(cache._c),
-         _i32(block_table, (B, pages), dev, "block_table"), pages,
-         _i32(lengths, (B,), dev, "lengths"), max_len, window,
-         D ** -0.5 if scale is None else float(scale), _f32(out, (B, heads, D), dev, "out", q.dtype),
-         None if workspace is None else workspace.data_ptr(),
-         0 if workspace is None else workspace.numel() * workspace.element_size())
+    pw, nw = (None, 0) if workspace is None else (workspace.data_ptr(), workspace.nbytes)
+    _run("d2moe_attn_decode", dev, stream, pq, qs, B, heads, cache._ref,
+         _arg(block_table, (B, pages), torch.int32, dev, "block_table"), pages,
+         _arg(lengths, (B,), torch.int32, dev, "lengths"), max_len, window,
+         D ** -0.5 if scale is None else scale, po, pw, nw)
     return out
 
 
@@ -631,22 +649,27 @@ def block_norm(x: torch.Tensor, y: torch.Tensor, eps: float = 1e-5, pre_weight=N
     x_scale * x + y_scale * gate * postnorm(y); returns h = prenorm(x) (h_dtype;
     None: only x is updated).  y [T][d]; gate [d] or [T][d] (rows may be
     strided); pre_weight, post_weight [d] float32 or None."""
-    T, d = x.shape
-    dev = x.device
-    px, py = _f32(x, (T, d), dev, "x"), _f32(y, (T, d), dev, "y", y.dtype)
+    shape, dev, f32 = x.shape, x.device, torch.float32
+    T, d = shape
+    px, py = _arg(x, shape, f32, dev, "x"), _arg(y, shape, y.dtype, dev, "y")
     pg, gs, gd = None, 0, D2MOE_F32
     if gate is not None:
-        if tuple(gate.shape) not in ((d,), (T, d)) or gate.device != dev or \
+        rows = gate.dim() == 2
+        if gate.shape != (shape if rows else (d,)) or gate.device != dev or \
                 (d > 1 and gate.stride(-1) != 1):
             raise ValueError(f"gate must be [d] or [T][d] = {(T, d)} on {dev}, rows contiguous")
-        pg, gs, gd = gate.data_ptr(), gate.stride(0) if gate.dim() == 2 else 0, _dtype_code(gate)
-    if h is None and h_dtype is not None:
-        h = _new((T, d), h_dtype, dev, stream)
-    _run("d2moe_block_norm", dev, stream, px, float(x_scale), py, _dtype_code(y), float(y_scale),
-         _f32(post_weight, (d,), dev, "post_weight"), pg, gd, gs,
-         _f32(pre_weight, (d,), dev, "pre_weight"), T, d, float(eps),
-         None if h is None else _f32(h, (T, d), dev, "h", h.dtype),
-         D2MOE_F32 if h is None else _dtype_code(h))
+        # one row alone has no stride
+        pg, gs, gd = gate.data_ptr(), gate.stride(0) if rows and T > 1 else 0, _dtype_code(gate)
+    ph, hd = None, D2MOE_F32
+    if h is not None:
+        ph, hd = _arg(h, shape, h.dtype, dev, "h"), _dtype_code(h)
+    elif h_dtype is not None:
+        h = _new(x, shape, h_dtype, stream)
+        ph, hd = h.data_ptr(), _dtype_code(h)
+    _run("d2moe_block_norm", dev, stream, px, x_scale, py, _dtype_code(y), y_scale,
+         None if post_weight is None else _arg(post_weight, (d,), f32, dev, "post_weight"), pg, gd,
+         gs, None if pre_weight is None else _arg(pre_weight, (d,), f32, dev, "pre_weight"), T, d,
+         eps, ph, hd)
     return h
 
 
