@@ -65,56 +65,78 @@ __device__ inline void store_row(void* p, bool bf, int64_t at, int n, const floa
   }
 }
 
-// Sum over the workgroup, the same on every thread; `part` is used once.
+template <int CTRL>
+__device__ inline float dpp_add(float v) {
+  return v + __int_as_float(
+                 __builtin_amdgcn_update_dpp(0, __float_as_int(v), CTRL, 0xf, 0xf, true));
+}
+
+// Sum over the workgroup, the same on every thread (rows of 16 lanes by DPP, the
+// four rows and the waves in order); `part` is used once.  The barrier is for LDS
+// alone, so that it does not wait for loads and stores under way.
 template <int THREADS>
 __device__ inline float group_sum(float v, float* part) {
-  for (int off = 32; off > 0; off >>= 1) v += __shfl_xor(v, off, 64);
+  v = dpp_add<0xB1>(v);   // lane ^ 1, lane ^ 2, halves of the row and the row mirrored
+  v = dpp_add<0x4E>(v);
+  v = dpp_add<0x141>(v);
+  v = dpp_add<0x140>(v);
+  const float r0 = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), 0));
+  const float r1 = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), 16));
+  const float r2 = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), 32));
+  const float r3 = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), 48));
+  v = (r0 + r1) + (r2 + r3);
   if constexpr (THREADS > 64) {
     if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = v;
-    __syncthreads();
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
+    __builtin_amdgcn_s_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
     v = 0.0f;
+#pragma unroll
     for (int k = 0; k < THREADS / 64; ++k) v += part[k];
   }
   return v;
 }
 
-// NPER runs of four values per thread (4 * NPER * THREADS >= d).
+// NPER runs of four values per thread (4 * NPER * THREADS >= d).  Everything is
+// loaded before the first sum: weights and gate loaded where they are used cost a
+// memory latency each (16 rows of 4096: 6.9 us).
 template <int THREADS, int NPER>
 __global__ __launch_bounds__(THREADS) void block_norm_kernel(NormArgs a) {
   __shared__ float part[2][THREADS / 64];
   const int64_t row = (int64_t)blockIdx.x * a.d;
   const int64_t grow = (int64_t)blockIdx.x * a.gate_stride;
-  float x[NPER][4], u[NPER][4];
+  float x[NPER][4], u[NPER][4], g[NPER][4], post[NPER][4], pre[NPER][4];
 #pragma unroll
   for (int i = 0; i < NPER; ++i) {
-    const int c = (threadIdx.x + i * THREADS) * 4;
-    load_row(a.y, a.y_bf, row + c, a.d - c, u[i]);
-    load_row(a.x, false, row + c, a.d - c, x[i]);
+    const int c = (threadIdx.x + i * THREADS) * 4, n = a.d - c;
+    load_row(a.y, a.y_bf, row + c, n, u[i]);
+    load_row(a.x, false, row + c, n, x[i]);
+    if (a.post_w) load_row(a.post_w, false, c, n, post[i]);
+    if (a.gate) load_row(a.gate, a.g_bf, grow + c, n, g[i]);
+    if (a.pre_w) load_row(a.pre_w, false, c, n, pre[i]);
   }
-  float inv = 1.0f;
   if (a.post_w) {
     float ss = 0.0f;
 #pragma unroll
     for (int i = 0; i < NPER; ++i)
 #pragma unroll
       for (int e = 0; e < 4; ++e) ss = fmaf(u[i][e], u[i][e], ss);
-    inv = 1.0f / sqrtf(group_sum<THREADS>(ss, part[0]) / (float)a.d + a.eps);
+    const float inv = 1.0f / sqrtf(group_sum<THREADS>(ss, part[0]) / (float)a.d + a.eps);
+#pragma unroll
+    for (int i = 0; i < NPER; ++i)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) u[i][e] = u[i][e] * inv * post[i][e];
+  }
+  if (a.gate) {
+#pragma unroll
+    for (int i = 0; i < NPER; ++i)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) u[i][e] *= g[i][e];
   }
   float ss = 0.0f;
 #pragma unroll
   for (int i = 0; i < NPER; ++i) {
     const int c = (threadIdx.x + i * THREADS) * 4;
-    float w[4], g[4];
-    if (a.post_w) {
-      load_row(a.post_w, false, c, a.d - c, w);
-#pragma unroll
-      for (int e = 0; e < 4; ++e) u[i][e] = u[i][e] * inv * w[e];
-    }
-    if (a.gate) {
-      load_row(a.gate, a.g_bf, grow + c, a.d - c, g);
-#pragma unroll
-      for (int e = 0; e < 4; ++e) u[i][e] *= g[e];
-    }
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
       x[i][e] = fmaf(a.y_scale, u[i][e], a.x_scale * x[i][e]);
@@ -123,40 +145,47 @@ __global__ __launch_bounds__(THREADS) void block_norm_kernel(NormArgs a) {
     store_row(a.x, false, row + c, a.d - c, x[i]);
   }
   if (!a.h) return;
-  inv = 1.0f / sqrtf(group_sum<THREADS>(ss, part[1]) / (float)a.d + a.eps);
+  const float inv = 1.0f / sqrtf(group_sum<THREADS>(ss, part[1]) / (float)a.d + a.eps);
 #pragma unroll
   for (int i = 0; i < NPER; ++i) {
     const int c = (threadIdx.x + i * THREADS) * 4;
-    float w[4];
 #pragma unroll
-    for (int e = 0; e < 4; ++e) x[i][e] *= inv;
-    if (a.pre_w) {
-      load_row(a.pre_w, false, c, a.d - c, w);
-#pragma unroll
-      for (int e = 0; e < 4; ++e) x[i][e] *= w[e];
-    }
+    for (int e = 0; e < 4; ++e) x[i][e] *= a.pre_w ? inv * pre[i][e] : inv;
     store_row(a.h, a.h_bf, row + c, a.d - c, x[i]);
   }
 }
 
+// Threads a row, by its runs of four values.  One run a thread leaves the shortest
+// chain; where rows fill the chip several times over, workgroups of 512 overlap
+// better.  Measured, bf16 with both norms and a gate for all rows, us (threads,
+// runs): 16 rows of 4096: (1024, 1) 3.73, (512, 2) 3.89, (256, 4) 5.16; 8192 rows of
+// 4096: 70.7, 62.4, 69.4; 16 rows of 8192: (1024, 2) 4.74, (512, 4) 5.61; 4096 rows
+// of 8192: 77.0, 73.3; 8192 rows of 2048: (512, 1) 33.1 (6.1 TB/s), (1024, 1) 52.6.
 hipError_t run_block_norm(const NormArgs& a, int T, hipStream_t s) {
-  const int n = (a.d + 3) / 4;  // runs of a row
+  const int n = (a.d + 3) / 4;
+  const bool few = T <= 256;  // one row a CU
   if (n <= 64)
     block_norm_kernel<64, 1><<<T, 64, 0, s>>>(a);
   else if (n <= 256)
     block_norm_kernel<256, 1><<<T, 256, 0, s>>>(a);
   else if (n <= 512)
-    block_norm_kernel<256, 2><<<T, 256, 0, s>>>(a);
+    block_norm_kernel<512, 1><<<T, 512, 0, s>>>(a);
+  else if (n <= 1024 && few)
+    block_norm_kernel<1024, 1><<<T, 1024, 0, s>>>(a);
   else if (n <= 1024)
-    block_norm_kernel<256, 4><<<T, 256, 0, s>>>(a);
+    block_norm_kernel<512, 2><<<T, 512, 0, s>>>(a);
+  else if (n <= 2048 && few)
+    block_norm_kernel<1024, 2><<<T, 1024, 0, s>>>(a);
+  else if (n <= 2048)
+    block_norm_kernel<512, 4><<<T, 512, 0, s>>>(a);
   else
-    block_norm_kernel<1024, 4><<<T, 1024, 0, s>>>(a);
+    block_norm_kernel<512, 8><<<T, 512, 0, s>>>(a);
   return hipGetLastError();
 }
 
 }  // namespace
 
-static_assert(kNormMax <= 4 * 4 * 1024, "a row fits the widest kernel");
+static_assert(kNormMax <= 4 * 8 * 512, "a row fits the widest kernel");
 
 hipError_t launch_block_norm(float* x, float x_scale, const void* y, d2moe_dtype yd, float y_scale,
                              const float* post_w, const void* gate, d2moe_dtype gd,

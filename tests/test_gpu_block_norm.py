@@ -55,6 +55,13 @@ def test_widths(d, y_dtype, h_dtype):
     check(3, d, y_dtype, h_dtype, True, True, "row f32", 0.9, 0.5, seed=d)
 
 
+@pytest.mark.parametrize("d", [2049, 4000, 4096, 4098, 8189])
+def test_many_rows(d):
+    """Row counts from which the wide rows take other workgroups."""
+    for T in (256, 257):
+        check(T, d, BF, BF, True, True, "token bf16", 0.9, 0.5, seed=T)
+
+
 @pytest.mark.parametrize("T", [1, 2, 65, 301])
 @pytest.mark.parametrize("gate", [None, "row bf16", "token bf16", "token f32",
                                   "token strided bf16", "token strided f32"])
