@@ -47,12 +47,21 @@ __device__ inline void load_row(const void* p, bool bf, int64_t at, int n, float
   }
 }
 
+// Rows that are many enough to leave the caches before they are read again are
+// stored past them (1024 rows of 4096 with a gate per token: 13.4 -> 12.5 us).
+template <bool PAST>
 __device__ inline void store_row(void* p, bool bf, int64_t at, int n, const float (&v)[4]) {
   if (n >= 4) {
-    if (bf)
-      *(h4*)((uint16_t*)p + at) = h4{f2bf(v[0]), f2bf(v[1]), f2bf(v[2]), f2bf(v[3])};
+    const h4 h = {f2bf(v[0]), f2bf(v[1]), f2bf(v[2]), f2bf(v[3])};
+    const f4 f = {v[0], v[1], v[2], v[3]};
+    if (bf && PAST)
+      __builtin_nontemporal_store(h, (h4*)((uint16_t*)p + at));
+    else if (bf)
+      *(h4*)((uint16_t*)p + at) = h;
+    else if (PAST)
+      __builtin_nontemporal_store(f, (f4*)((float*)p + at));
     else
-      *(f4*)((float*)p + at) = f4{v[0], v[1], v[2], v[3]};
+      *(f4*)((float*)p + at) = f;
   } else if (n > 0) {
 #pragma unroll
     for (int e = 0; e < 3; ++e)
@@ -97,23 +106,28 @@ __device__ inline float group_sum(float v, float* part) {
   return v;
 }
 
-// NPER runs of four values per thread (4 * NPER * THREADS >= d).  Everything is
-// loaded before the first sum: weights and gate loaded where they are used cost a
-// memory latency each (16 rows of 4096: 6.9 us).
-template <int THREADS, int NPER>
+// NPER runs of four values per thread (4 * NPER * THREADS >= d).  AHEAD: everything
+// is loaded before the first sum, for few rows, where weights and gate loaded at
+// their use cost a memory latency each (16 rows of 4096: 6.9 us, ahead 3.7).  For
+// many rows the registers that this takes cost more than other rows hide (4096
+// rows of 8192: 108 us, at their use 82).
+template <int THREADS, int NPER, bool AHEAD, bool PAST>
 __global__ __launch_bounds__(THREADS) void block_norm_kernel(NormArgs a) {
   __shared__ float part[2][THREADS / 64];
   const int64_t row = (int64_t)blockIdx.x * a.d;
   const int64_t grow = (int64_t)blockIdx.x * a.gate_stride;
   float x[NPER][4], u[NPER][4], g[NPER][4], post[NPER][4], pre[NPER][4];
+  auto load_rest = [&](int i, int c, int n) {
+    if (a.post_w) load_row(a.post_w, false, c, n, post[i]);
+    if (a.gate) load_row(a.gate, a.g_bf, grow + c, n, g[i]);
+    if (a.pre_w) load_row(a.pre_w, false, c, n, pre[i]);
+  };
 #pragma unroll
   for (int i = 0; i < NPER; ++i) {
     const int c = (threadIdx.x + i * THREADS) * 4, n = a.d - c;
     load_row(a.y, a.y_bf, row + c, n, u[i]);
     load_row(a.x, false, row + c, n, x[i]);
-    if (a.post_w) load_row(a.post_w, false, c, n, post[i]);
-    if (a.gate) load_row(a.gate, a.g_bf, grow + c, n, g[i]);
-    if (a.pre_w) load_row(a.pre_w, false, c, n, pre[i]);
+    if constexpr (AHEAD) load_rest(i, c, n);
   }
   if (a.post_w) {
     float ss = 0.0f;
@@ -123,15 +137,21 @@ __global__ __launch_bounds__(THREADS) void block_norm_kernel(NormArgs a) {
       for (int e = 0; e < 4; ++e) ss = fmaf(u[i][e], u[i][e], ss);
     const float inv = 1.0f / sqrtf(group_sum<THREADS>(ss, part[0]) / (float)a.d + a.eps);
 #pragma unroll
-    for (int i = 0; i < NPER; ++i)
+    for (int i = 0; i < NPER; ++i) {
+      const int c = (threadIdx.x + i * THREADS) * 4;
+      if constexpr (!AHEAD) load_row(a.post_w, false, c, a.d - c, post[i]);
 #pragma unroll
       for (int e = 0; e < 4; ++e) u[i][e] = u[i][e] * inv * post[i][e];
+    }
   }
   if (a.gate) {
 #pragma unroll
-    for (int i = 0; i < NPER; ++i)
+    for (int i = 0; i < NPER; ++i) {
+      const int c = (threadIdx.x + i * THREADS) * 4;
+      if constexpr (!AHEAD) load_row(a.gate, a.g_bf, grow + c, a.d - c, g[i]);
 #pragma unroll
       for (int e = 0; e < 4; ++e) u[i][e] *= g[i][e];
+    }
   }
   float ss = 0.0f;
 #pragma unroll
@@ -142,50 +162,61 @@ __global__ __launch_bounds__(THREADS) void block_norm_kernel(NormArgs a) {
       x[i][e] = fmaf(a.y_scale, u[i][e], a.x_scale * x[i][e]);
       ss = fmaf(x[i][e], x[i][e], ss);  // zero past the row
     }
-    store_row(a.x, false, row + c, a.d - c, x[i]);
+    store_row<PAST>(a.x, false, row + c, a.d - c, x[i]);
   }
   if (!a.h) return;
   const float inv = 1.0f / sqrtf(group_sum<THREADS>(ss, part[1]) / (float)a.d + a.eps);
 #pragma unroll
   for (int i = 0; i < NPER; ++i) {
     const int c = (threadIdx.x + i * THREADS) * 4;
+    if constexpr (!AHEAD)
+      if (a.pre_w) load_row(a.pre_w, false, c, a.d - c, pre[i]);
 #pragma unroll
     for (int e = 0; e < 4; ++e) x[i][e] *= a.pre_w ? inv * pre[i][e] : inv;
-    store_row(a.h, a.h_bf, row + c, a.d - c, x[i]);
+    store_row<PAST>(a.h, a.h_bf, row + c, a.d - c, x[i]);
   }
 }
 
-// Threads a row, by its runs of four values.  One run a thread leaves the shortest
-// chain; where rows fill the chip several times over, workgroups of 512 overlap
-// better.  Measured, bf16 with both norms and a gate for all rows, us (threads,
-// runs): 16 rows of 4096: (1024, 1) 3.73, (512, 2) 3.89, (256, 4) 5.16; 8192 rows of
-// 4096: 70.7, 62.4, 69.4; 16 rows of 8192: (1024, 2) 4.74, (512, 4) 5.61; 4096 rows
-// of 8192: 77.0, 73.3; 8192 rows of 2048: (512, 1) 33.1 (6.1 TB/s), (1024, 1) 52.6.
+template <int THREADS, int NPER, bool AHEAD, bool PAST>
+void run_block_norm_n(const NormArgs& a, int T, hipStream_t s) {
+  block_norm_kernel<THREADS, NPER, AHEAD, PAST><<<T, THREADS, 0, s>>>(a);
+}
+
+// Threads a row, by its runs of four values: one run a thread leaves the shortest
+// chain; where rows fill the chip several times over, more runs for wide rows.
+// Measured, bf16 with both norms and one gate row, us (threads, runs): 16 rows of
+// 4096: (1024, 1) 3.7, (512, 2) 3.9, (256, 4) 5.2; 8192 rows of 4096: 85.5, 82.6
+// (4.9 TB/s), 92.2; 16 rows of 8192: (1024, 2) 4.7, (512, 4) 5.6; 4096 rows of
+// 8192: 81.5, 99.2; 2048 rows of 16384: (1024, 4) 94, (512, 8) 135.
 hipError_t run_block_norm(const NormArgs& a, int T, hipStream_t s) {
   const int n = (a.d + 3) / 4;
-  const bool few = T <= 256;  // one row a CU
+  const bool few = T <= 256;                        // one row a CU
+  const bool held = (int64_t)T * a.d <= (4 << 20);  // x stays in the L2s (4 MB a XCD)
   if (n <= 64)
-    block_norm_kernel<64, 1><<<T, 64, 0, s>>>(a);
+    held ? run_block_norm_n<64, 1, true, false>(a, T, s) : run_block_norm_n<64, 1, true, true>(a, T, s);
   else if (n <= 256)
-    block_norm_kernel<256, 1><<<T, 256, 0, s>>>(a);
+    held ? run_block_norm_n<256, 1, true, false>(a, T, s)
+         : run_block_norm_n<256, 1, true, true>(a, T, s);
   else if (n <= 512)
-    block_norm_kernel<512, 1><<<T, 512, 0, s>>>(a);
-  else if (n <= 1024 && few)
-    block_norm_kernel<1024, 1><<<T, 1024, 0, s>>>(a);
+    held ? run_block_norm_n<512, 1, true, false>(a, T, s)
+         : run_block_norm_n<512, 1, true, true>(a, T, s);
   else if (n <= 1024)
-    block_norm_kernel<512, 2><<<T, 512, 0, s>>>(a);
-  else if (n <= 2048 && few)
-    block_norm_kernel<1024, 2><<<T, 1024, 0, s>>>(a);
+    few    ? run_block_norm_n<1024, 1, true, false>(a, T, s)
+    : held ? run_block_norm_n<512, 2, false, false>(a, T, s)
+           : run_block_norm_n<512, 2, false, true>(a, T, s);
   else if (n <= 2048)
-    block_norm_kernel<512, 4><<<T, 512, 0, s>>>(a);
+    few    ? run_block_norm_n<1024, 2, true, false>(a, T, s)
+    : held ? run_block_norm_n<1024, 2, false, false>(a, T, s)
+           : run_block_norm_n<1024, 2, false, true>(a, T, s);
   else
-    block_norm_kernel<512, 8><<<T, 512, 0, s>>>(a);
+    held ? run_block_norm_n<1024, 4, false, false>(a, T, s)
+         : run_block_norm_n<1024, 4, false, true>(a, T, s);
   return hipGetLastError();
 }
 
 }  // namespace
 
-static_assert(kNormMax <= 4 * 8 * 512, "a row fits the widest kernel");
+static_assert(kNormMax <= 4 * 4 * 1024, "a row fits the widest kernel");
 
 hipError_t launch_block_norm(float* x, float x_scale, const void* y, d2moe_dtype yd, float y_scale,
                              const float* post_w, const void* gate, d2moe_dtype gd,

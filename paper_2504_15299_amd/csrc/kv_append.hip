@@ -33,7 +33,28 @@ struct AppendArgs {
 // One thread takes N values of the first half of a head and the N that go
 // with them in the second.  Workgroups walk a token's heads along x (queries,
 // keys, values), tokens along y.
-template <typename TI, typename TO, int N>
+// PAST: many tokens' rows leave the caches before they are read again and are
+// stored past them (1024 tokens, 32 and 8 heads of 128, bf16: 7.9 -> 6.6 us; 8192:
+// 41.8 -> 41.0 us, 4.9 TB/s).
+template <bool PAST, typename T>
+__device__ inline void put(T* p, const T& v) {
+  if constexpr (PAST) {
+    // 32-byte packs are stored in two
+    constexpr int kWords = sizeof(T) < 16 ? sizeof(T) / 4 : 4;
+    typedef uint32_t words __attribute__((ext_vector_type(kWords)));
+    struct Parts {
+      words w[sizeof(T) / 4 / kWords];
+    };
+    const Parts x = __builtin_bit_cast(Parts, v);
+#pragma unroll
+    for (int i = 0; i < (int)(sizeof(T) / 4 / kWords); ++i)
+      __builtin_nontemporal_store(x.w[i], (words*)p + i);
+  } else {
+    *p = v;
+  }
+}
+
+template <typename TI, typename TO, int N, bool PAST>
 __global__ __launch_bounds__(kAppendThreads) void kv_append_kernel(AppendArgs a) {
   const int half = a.D / 2, per = half / N;
   const int item = blockIdx.x * kAppendThreads + threadIdx.x;
@@ -85,23 +106,28 @@ __global__ __launch_bounds__(kAppendThreads) void kv_append_kernel(AppendArgs a)
         from_f(to_f(y.v[e]), w.v[e]);
       }
     }
-    *(Pack<TO, N>*)(dst + i) = u;
-    *(Pack<TO, N>*)(dst + half + i) = w;
+    put<PAST>((Pack<TO, N>*)(dst + i), u);
+    put<PAST>((Pack<TO, N>*)(dst + half + i), w);
   }
+}
+
+template <typename TI, typename TO, int N>
+hipError_t run_append_n(const AppendArgs& a, hipStream_t s) {
+  const int items = (a.Hq + 2 * a.H) * (a.D / 2 / N);
+  const dim3 grid((items + kAppendThreads - 1) / kAppendThreads, a.N < 65535 ? a.N : 65535);
+  if (a.N <= 256)
+    kv_append_kernel<TI, TO, N, false><<<grid, kAppendThreads, 0, s>>>(a);
+  else
+    kv_append_kernel<TI, TO, N, true><<<grid, kAppendThreads, 0, s>>>(a);
+  return hipGetLastError();
 }
 
 template <typename TI, typename TO>
 hipError_t run_append(const AppendArgs& a, hipStream_t s) {
   // 16-byte accesses of bf16 need halves of 8 values; 4 always fit (D % 8 == 0)
-  const bool wide = a.D % 16 == 0 && (sizeof(TI) == 2 || sizeof(TO) == 2);
-  const int n = wide ? 8 : 4;
-  const int items = (a.Hq + 2 * a.H) * (a.D / 2 / n);
-  const dim3 grid((items + kAppendThreads - 1) / kAppendThreads, a.N < 65535 ? a.N : 65535);
-  if (wide)
-    kv_append_kernel<TI, TO, 8><<<grid, kAppendThreads, 0, s>>>(a);
-  else
-    kv_append_kernel<TI, TO, 4><<<grid, kAppendThreads, 0, s>>>(a);
-  return hipGetLastError();
+  if constexpr (sizeof(TI) == 2 || sizeof(TO) == 2)
+    if (a.D % 16 == 0) return run_append_n<TI, TO, 8>(a, s);
+  return run_append_n<TI, TO, 4>(a, s);
 }
 
 }  // namespace
