@@ -101,6 +101,11 @@ def main():
     ap.add_argument("--stack-steps", type=int, default=128,
                     help="also run the 32-layer decoder stack of MoE layers, 64 sequences, "
                          "this many decode steps (0: skip)")
+    ap.add_argument("--stack-context", type=int, default=0,
+                    help="also run that stack with attention before every MoE layer (4-bit "
+                         "projections, 32 query and 8 key heads of 128, paged cache), the "
+                         "sequences this many tokens long at the start (0: skip)")
+    ap.add_argument("--stack-layers", type=int, default=32, help="layers of the stacks")
     ap.add_argument("--variant-steps", type=int, default=40,
                     help="also time batch-16 decode under the paper's two nests (b 2-4, b 5-8) "
                          "and the LLaMA2-13B-shaped dense FFN (0: skip)")
@@ -424,7 +429,7 @@ def main():
                 "hbm_frac": round(gbps / HBM_PEAK_GBPS, 4), "alg_GFLOP": round(flop / 1e9, 2),
                 "TFLOPs": round(tflops, 1), "mfma_frac": round(tflops / MFMA_BF16_PEAK_TFLOPS, 4)}
 
-    def run_stack(steps, n_layers=32, T=64, eps=1e-5):
+    def run_stack(steps, n_layers=32, T=64, eps=1e-5, context=0):
         """Decoder stack: n_layers Mixtral-8x7B-shaped MoE layers, each block
         x <- x + MoE_l(rmsnorm(x)) (attention absent), all layers resident,
         MWQ group 128 nested to 8 bits; 64 sequences, each a request with one
@@ -432,8 +437,36 @@ def main():
         step feeds the previous step's final hidden state.  Reports tokens/s
         over all steps and the algorithmic HBM bytes of a step (every layer's
         active experts at their largest bit-width, from the last step's
-        routing)."""
+        routing).  With a context, every layer has attention before the MoE:
+        x <- x + o(attn(qkv(rmsnorm(x)))), 4-bit projections, the sequences
+        `context` tokens long at the start, their caches in pages of 16
+        tokens in random places; the step's bytes then include the
+        projections and the cache rows attended."""
         stack = []
+        attn, page, heads, kv_heads, dim = [], 16, 32, 8, 128
+        if context:
+            width = -(-(context + steps) // page)
+            lengths = torch.full((T,), context, dtype=torch.int32, device=dev)
+            gen.manual_seed(77)
+            pages = torch.randperm(T * width, generator=gen, device=dev).int().view(T, width)
+            ang = torch.arange(width * page, dtype=torch.float64)[:, None] * \
+                1e4 ** (-torch.arange(dim // 2, dtype=torch.float64) * 2 / dim)
+            cos, sin = ang.cos().float().to(dev), ang.sin().float().to(dev)
+            for l in range(n_layers):
+                gen.manual_seed(9000 + l)
+                cache = api.KVCache.empty(T * width, page, kv_heads, dim, device=dev)
+                cache.k.normal_(generator=gen)
+                cache.v.normal_(generator=gen)
+                lin = [api.linear_pack(torch.randn((r, c), generator=gen, device=dev) * 0.02,
+                                       api.Linear.empty(r, c, g, device=dev))
+                       for r, c in (((heads + 2 * kv_heads) * dim, d), (d, heads * dim))]
+                attn.append((cache, *lin))
+            qkv = torch.empty((T, (heads + 2 * kv_heads) * dim), dtype=torch.bfloat16, device=dev)
+            q, k_new, v_new = qkv.view(T, -1, dim).split([heads, kv_heads, kv_heads], dim=1)
+            q_rot = torch.empty((T, heads, dim), dtype=torch.bfloat16, device=dev)
+            att = torch.empty_like(q_rot)
+            attn_ws = torch.empty(api.attn_decode_workspace(T, heads, attn[0][0], width * page),
+                                  dtype=torch.uint8, device=dev)
         for l in range(n_layers):
             w13 = api.MWQ.empty(E, 2 * f, d, g, b_min, b_max, device=dev)
             w2 = api.MWQ.empty(E, d, f, g, b_min, b_max, device=dev)
@@ -459,7 +492,18 @@ def main():
         ws = torch.empty(api.moe_forward_workspace(T, d, f, E, k), dtype=torch.uint8, device=dev)
 
         def decode_step():
-            for w13, w2, Wg, r in stack:
+            if context:
+                lengths.add_(1)
+                position = lengths - 1
+            for l, (w13, w2, Wg, r) in enumerate(stack):
+                if context:
+                    cache, w_qkv, w_o = attn[l]
+                    api.linear_forward(h, w_qkv, y=qkv)
+                    api.kv_append(q, k_new, v_new, cache, pages, position, cos=cos, sin=sin,
+                                  q_out=q_rot)
+                    api.attn_decode(q_rot, cache, pages, lengths, out=att, workspace=attn_ws)
+                    api.linear_forward(att.view(T, -1), w_o, y=y)
+                    api.block_norm(x, y, eps, h=h)
                 api.route(h, Wg, None, k, req, table, b_min, b_max, out=r)
                 api.moe_forward(h, w13, w2, r, k, out=y, workspace=ws)
                 api.residual_rmsnorm(x, y, eps, h=h)
@@ -467,6 +511,8 @@ def main():
         api.residual_rmsnorm(x, None, eps, h=h)
         warm(lambda i: decode_step(), 1)   # warm-up steps, then restart from x0
         x.copy_(x0)
+        if context:
+            lengths.fill_(context)
         api.residual_rmsnorm(x, None, eps, h=h)
         torch.cuda.synchronize()
         t_start = torch.cuda.Event(enable_timing=True)
@@ -481,12 +527,16 @@ def main():
         for w13, w2, Wg, r in stack:
             for b in r.expert_maxbit.cpu().numpy():
                 step_bytes += mwq_bytes(2 * f, d, g, b_min, int(b)) + mwq_bytes(d, f, g, b_min, int(b))
+        for cache, w_qkv, w_o in attn:
+            step_bytes += w_qkv.nbytes() + w_o.nbytes()
+            step_bytes += int(T * (context + (steps + 1) / 2) * kv_heads * dim * 2 * 2)
         gbps = step_bytes * steps / (ms * 1e-3) / 1e9
         finite = bool(torch.isfinite(x).all().item())
-        del stack
+        del stack, attn
         torch.cuda.empty_cache()
+        about = f"attention over {context} tokens and more" if context else "attention absent"
         return {"workload": f"{n_layers}-layer decoder stack of Mixtral-8x7B-shaped MoE layers "
-                            f"(x <- x + MoE(rmsnorm(x)), attention absent), {T} sequences x "
+                            f"(x <- x + MoE(rmsnorm(x)), {about}), {T} sequences x "
                             f"{steps} decode steps, per-sequence bit tier from {{2,4,8}}, "
                             f"group 128, 8-bit nest, all layers resident",
                 "layers": n_layers, "sequences": T, "steps": steps,
@@ -834,7 +884,10 @@ def main():
     tiny = run_tiny(args.tiny_steps) if args.tiny_steps > 0 else None
     prefill = run_prefill(args.prefill_steps, 2) if args.prefill_steps > 0 else None
     fine = run_fine(args.fine_steps, 2) if args.fine_steps > 0 else None
-    stack_res = run_stack(args.stack_steps) if args.stack_steps > 0 else None
+    stack_res = run_stack(args.stack_steps, args.stack_layers) if args.stack_steps > 0 else None
+    attn_res = None
+    if args.stack_context > 0 and args.stack_steps > 0:
+        attn_res = run_stack(args.stack_steps, args.stack_layers, context=args.stack_context)
     variants = None
     if args.variant_steps > 0:
         vs = args.variant_steps
@@ -905,6 +958,8 @@ def main():
         "cpu_baseline": cpu,
         "pack_seconds": round(pack_s, 2),
     }
+    if attn_res is not None:
+        line["stack_attention"] = attn_res
     print(json.dumps(line), flush=True)
 
 
