@@ -354,17 +354,25 @@ hipError_t run_linear_g(const LinArgs& a, hipStream_t s) {
   return hipGetLastError();
 }
 
-// The division of the work goes by the number of 16 x 16 tiles of the result.
-// Up to one per CU, a workgroup takes one tile and its waves divide the columns;
-// with more, workgroups of 2, 4 and 8 row tiles share the activations (whose
-// reading from L2 bounds the kernel otherwise) while one round of workgroups
-// still fills the chip.  Measured, bf16, 4096 columns, group 128, us (R, S):
-//   4096 rows x 16 (256 tiles):  1, 8: 6.1   2, 4: 7.3   4, 4: 8.7   8, 2: 12.5
-//   6144 rows x 16 (384 tiles):  1, 8: 8.9   2, 4: 7.6   4, 4: 8.8   8, 2: 12.6
-//   4096 rows x 64 (1024 tiles): 2, 4: 10.6  4, 4: 9.3   8, 2: 12.5
-//   32000 rows x 16:             4, 4: 18.1  8, 2: 16.7
-//   32000 rows x 64:             8, 2: 55.8; 32 tokens, 8, 2: 35.4; 64 tokens, RT 2, 4, 2: 30.2
-// Binary32 activations take three times the LDS and twice the time.
+// The division of the work.  Workgroups of 128 rows by 64 or 32 tokens reuse most,
+// and are taken where three quarters of the CUs get one.  Otherwise it goes by
+// the number of 16 x 16 tiles of the result: up to one per CU, a workgroup takes
+// one tile and its waves divide the columns; with more, 2, 4 and 8 row tiles share
+// the activations (whose reading from L2 bounds the kernel otherwise) while one
+// round of workgroups fills the chip.  Measured, bf16, 4096 columns, group 128, us:
+//   R, S of 16-token workgroups         1, 8   2, 4   4, 4   8, 2
+//   4096 rows x 16 (256 tiles)           6.1    7.3    8.7   12.5
+//   6144 rows x 16 (384 tiles)           8.9    7.6    8.8   12.6
+//   4096 rows x 64 (1024 tiles)                10.6    9.3   12.5
+//   6144 rows x 64 (1536 tiles)                15.4   16.3   12.6
+//   32000 rows x 16                                   18.1   16.7
+//   tokens of a workgroup of 128 rows      16     32     64
+//   6144 rows x 64 (192, 96, 48 of them) 12.6   16.1   27.3
+//   16384 rows x 64 (512, 256, 128)             17.8   29.1
+//   32000 rows x 64 (1000, 500, 250)     55.8   35.7   29.5
+// What bounds the last (2.5 TB/s, 0.57 PFLOP/s) is issue: the vector ALU is busy
+// for 48 % of the cycles, the matrix pipe for 24 %, two waves a SIMD.  Binary32
+// activations take three times the LDS and products.
 constexpr int kCus = 256;
 
 template <int NU, int GB>
@@ -392,12 +400,14 @@ hipError_t run_linear_32(const LinArgs& a, int64_t tiles, hipStream_t s) {
 template <int GB>
 hipError_t run_linear(const LinArgs& a, bool x_bf, hipStream_t s) {
   const int64_t tiles = (int64_t)a.RB * ((a.T + 15) / 16);
-  if constexpr (GB < 4)  // as above
-    if (tiles > 8 * kCus && a.T > 16) {
-      if (!x_bf) return run_linear_g<float, 2, 8, GB == 1 ? 2 : 1, 4, 2, GB>(a, s);
-      if (a.T <= 32) return run_linear_g<uint16_t, 2, 8, 1, 8, 2, GB>(a, s);
+  if constexpr (GB < 4) {  // as above
+    const int64_t rows = (a.RB + 7) / 8, enough = kCus * 3 / 4;
+    if (x_bf && a.T > 32 && rows * ((a.T + 63) / 64) >= enough)
       return run_linear_g<uint16_t, 4, 16, 2, 4, 2, GB>(a, s);
-    }
+    if (a.T > 16 && rows * ((a.T + 31) / 32) >= enough)
+      return x_bf ? run_linear_g<uint16_t, 2, 8, 1, 8, 2, GB>(a, s)
+                  : run_linear_g<float, 2, 8, GB == 1 ? 2 : 1, 4, 2, GB>(a, s);
+  }
   if (a.T <= 4) return x_bf ? run_linear_16<1, GB>(a, tiles, s) : run_linear_32<1, GB>(a, tiles, s);
   if (a.T <= 8) return x_bf ? run_linear_16<2, GB>(a, tiles, s) : run_linear_32<2, GB>(a, tiles, s);
   return x_bf ? run_linear_16<4, GB>(a, tiles, s) : run_linear_32<4, GB>(a, tiles, s);

@@ -85,6 +85,22 @@ def test_shapes(rows, cols, group):
     check(19, rows, cols, group, F32, BF, bias=False, seed=rows + cols)
 
 
+# row counts from which workgroups of more rows and tokens are taken
+@pytest.mark.parametrize("T,rows", [(17, 24000), (33, 24590), (65, 12290), (100, 6150), (4, 8200),
+                                    (7, 16500), (16, 33000), (130, 1040)])
+@pytest.mark.parametrize("cols,group", [(160, 32), (192, 64), (384, 128)])
+@pytest.mark.parametrize("x_dtype", [BF, F32])
+def test_many_rows(T, rows, cols, group, x_dtype):
+    check(T, rows, cols, group, x_dtype, x_dtype, bias=True, seed=T)
+
+
+@pytest.mark.parametrize("T", [1, 3, 5, 20])
+@pytest.mark.parametrize("x_dtype", [BF, F32])
+def test_long_rows(T, x_dtype):
+    check(T, 40, 14336, 128, x_dtype, x_dtype, bias=False, seed=T)
+    check(T, 40, 8256, 64, x_dtype, x_dtype, bias=False, seed=T)
+
+
 def test_activations_with_a_large_mean():
     check(16, 64, 512, 128, BF, BF, bias=False, shift=30.0)
     check(16, 64, 512, 128, F32, F32, bias=False, shift=30.0)
