@@ -400,7 +400,8 @@ d2moe_status d2moe_attn_decode(const void* q, int64_t q_stride, int32_t B, int32
                                size_t ws_bytes, void* stream) {
   if (!cache_ok(cache) ||
       !attn_shape_ok(B, q_heads, cache->n_heads, cache->head_dim, max_len) || max_pages < 0 ||
-      window < 0 || !(scale - scale == 0.0f))
+      window < 0 || !(scale - scale == 0.0f) ||
+      (int64_t)max_pages * cache->page_size > (1 << 30))
     return D2MOE_EINVAL;
   if (B == 0) return D2MOE_OK;
   const int64_t step = 16 / dtype_size(cache->dtype);

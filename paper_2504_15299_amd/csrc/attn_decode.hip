@@ -31,9 +31,9 @@ typedef float f4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u4 __attribute__((ext_vector_type(4)));
 
 constexpr int kHeadTile = 16;    // query heads of a workgroup
-constexpr int kKeysAhead = 1024; // keys whose row offsets are held in LDS at a time
-constexpr int kWholeKeys = 512;  // up to here a workgroup takes a unit whole,
-constexpr int kManyUnits = 96;   // up to twice as many with that many units
+constexpr int kChunk = 512;      // keys whose row offsets are worked out at a time
+constexpr int kWholeKeys = 1024;  // up to here a workgroup takes a unit whole,
+constexpr int kManyUnits = 256;   // up to twice as many with that many units
 constexpr int kMaxSplitUnits = 2048;
 constexpr int kSplitSeqs = 256;  // most sequences of a call whose keys are split
 constexpr int kMinShare = 4;     // tiles
@@ -118,43 +118,78 @@ __device__ inline f4 mma(float a, float b, f4 c) {
   return d;
 }
 
-// The tile products of one cache type: TK keys a step, a lane's share of the
-// key rows (K), of the value rows (V) and of Q.  A lane loads VE consecutive
-// values of a value row, dimensions 16 VE h + VE (l % 16) + 0 .. VE - 1, so that
-// 16 lanes read a run of 16 VE values; element i of that run is the row l % 16
-// of value product (h, i).  PAD: head_dim D is below DP; K and Q are zero past
-// D, value loads past D read the row's start and their results are not used.
+// The tile products of one cache type: TK keys a step, a lane's share of the key
+// rows as loaded (K), of the value rows (V) and of Q.  Head dimensions past D, where
+// it is below DP (PAD), are zero in K and Q; value loads past D read the row's
+// start and their results are not used.
+//
+// An operand of the key product has neighbouring lanes in neighbouring rows, and
+// loads of that pattern take the L1 four times as long as loads of whole rows
+// (a workgroup alone read 14 bytes a cycle).  Key rows are therefore loaded as
+// they lie, CPR lanes of 16 bytes a row, and turned in LDS by the wave that uses
+// them: chunk c of row r lies at r CPR + (c ^ swizzle(r)), so that 16 lanes meet 16
+// different bank groups both writing (one row) and reading (16 rows, one c).
+//
+// Of a value row a lane loads VE consecutive values, dimensions 16 VE h + VE (l % 16)
+// + 0 .. VE - 1, so that 16 lanes read a run of 16 VE values; element i of that run
+// is the row l % 16 of value product (h, i).
+template <int CPR>
+__device__ inline int swizzle(int row) {
+  return CPR >= 16 ? row & 15 : (row >> 1) & 7;
+}
+
+template <typename E, int DP, int TK_>
+struct KeyRows {
+  static constexpr int TK = TK_, PER = 16 / sizeof(E), CPR = DP / PER;
+  static constexpr int NK = TK * CPR / 64, KS = CPR / 4;  // loads of a lane; operands of 16 rows
+  struct K { u4 f[NK]; };
+  struct Lds { u4 x[TK * CPR]; };
+  static_assert(CPR >= 8 && TK * CPR % 64 == 0, "a load covers whole rows");
+
+  template <bool PAD>
+  __device__ static void load(K& o, const E* k, const int64_t* off, int lane, int D) {
+#pragma unroll
+    for (int j = 0; j < NK; ++j) {
+      const int x = 64 * j + lane, row = x / CPR;
+      int c = (x % CPR ^ swizzle<CPR>(row)) * PER;
+      if (PAD && c >= D) c = 0;
+      const int64_t at = off[row];
+      o.f[j] = *(const u4*)(k + (at < 0 ? 0 : at) + c);
+    }
+  }
+  __device__ static void store(Lds& l, const K& k, int lane) {
+#pragma unroll
+    for (int j = 0; j < NK; ++j) l.x[64 * j + lane] = k.f[j];
+  }
+  // operand s of tile t: row 16 t + l % 16, chunk 4 s + l / 16
+  template <bool PAD>
+  __device__ static u4 operand(const Lds& l, int t, int s, int lane, int D) {
+    const int row = 16 * t + (lane & 15), c = 4 * s + (lane >> 4);
+    const u4 v = l.x[row * CPR + (c ^ swizzle<CPR>(row))];
+    return PAD && c * PER >= D ? u4{0, 0, 0, 0} : v;
+  }
+};
+
 template <typename T, int DP, bool PAD>
 struct Tile;
 
 template <int DP, bool PAD>
-struct Tile<uint16_t, DP, PAD> {
-  static constexpr int TK = 32, VE = DP >= 128 ? 8 : 4, H = DP / (16 * VE), KS = DP / 32;
+struct Tile<uint16_t, DP, PAD> : KeyRows<uint16_t, DP, 32> {
+  using Rows = KeyRows<uint16_t, DP, 32>;
+  using typename Rows::Lds;
+  static constexpr int VE = DP >= 128 ? 8 : 4, H = DP / (16 * VE), KS = Rows::KS;
   static constexpr int NV = 8;  // value rows (keys) of a lane
   struct Q { u4 f[KS]; };
-  struct K { u4 f[2][KS]; };
   struct V { uint32_t f[NV][H][VE / 2]; };
 
   __device__ static int key_of(int j, int q) { return j < 4 ? 4 * q + j : 12 + 4 * q + j; }
 
-  __device__ static u4 chunk(const uint16_t* p, int c, int D) {
-    if (PAD && c >= D) return u4{0, 0, 0, 0};
-    return *(const u4*)(p + c);
-  }
   __device__ static void load_q(Q& o, const uint16_t* row, int q, int D, bool live) {
 #pragma unroll
     for (int s = 0; s < KS; ++s) {
+      const int c = 32 * s + 8 * q;
       o.f[s] = u4{0, 0, 0, 0};
-      if (live) o.f[s] = chunk(row, 32 * s + 8 * q, D);
-    }
-  }
-  __device__ static void load_k(K& o, const uint16_t* k, const int64_t* off, int lane, int D) {
-#pragma unroll
-    for (int t = 0; t < 2; ++t) {
-      const int64_t at = off[16 * t + (lane & 15)];
-      const uint16_t* row = k + (at < 0 ? 0 : at);
-#pragma unroll
-      for (int s = 0; s < KS; ++s) o.f[t][s] = chunk(row, 32 * s + 8 * (lane >> 4), D);
+      if (live && (!PAD || c < D)) o.f[s] = *(const u4*)(row + c);
     }
   }
   __device__ static void load_v(V& o, const uint16_t* v, const int64_t (&at)[NV], int lane, int D) {
@@ -185,12 +220,17 @@ struct Tile<uint16_t, DP, PAD> {
 #pragma unroll
         for (int d = 0; d < VE / 2; ++d) o.f[j][h][d] = at[j] < 0 ? 0u : o.f[j][h][d];
   }
-  __device__ static void scores(float (&s)[NV], const K& k, const Q& q) {
+  __device__ static void scores(float (&s)[NV], const Lds& k, const Q& q, int lane, int D) {
+    u4 x[2][KS];
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+      for (int c = 0; c < KS; ++c) x[t][c] = Rows::template operand<PAD>(k, t, c, lane, D);
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
       f4 acc = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-      for (int c = 0; c < KS; ++c) acc = mma(k.f[t][c], q.f[c], acc);
+      for (int c = 0; c < KS; ++c) acc = mma(x[t][c], q.f[c], acc);
 #pragma unroll
       for (int i = 0; i < 4; ++i) s[4 * t + i] = acc[i];
     }
@@ -229,31 +269,23 @@ struct Tile<uint16_t, DP, PAD> {
 };
 
 template <int DP, bool PAD>
-struct Tile<float, DP, PAD> {
-  static constexpr int TK = 16, VE = 4, H = DP / 64, KS = DP / 16;
+struct Tile<float, DP, PAD> : KeyRows<float, DP, 16> {
+  using Rows = KeyRows<float, DP, 16>;
+  using typename Rows::Lds;
+  static constexpr int VE = 4, H = DP / 64, KS = Rows::KS;
   static constexpr int NV = 4;
   struct Q { f4 f[KS]; };
-  struct K { f4 f[KS]; };
   struct V { f4 f[NV][H]; };
 
   __device__ static int key_of(int j, int q) { return 4 * q + j; }
 
-  __device__ static f4 chunk(const float* p, int c, int D) {
-    if (PAD && c >= D) return f4{0.0f, 0.0f, 0.0f, 0.0f};
-    return *(const f4*)(p + c);
-  }
   __device__ static void load_q(Q& o, const float* row, int q, int D, bool live) {
 #pragma unroll
     for (int s = 0; s < KS; ++s) {
+      const int c = 16 * s + 4 * q;
       o.f[s] = f4{0.0f, 0.0f, 0.0f, 0.0f};
-      if (live) o.f[s] = chunk(row, 16 * s + 4 * q, D);
+      if (live && (!PAD || c < D)) o.f[s] = *(const f4*)(row + c);
     }
-  }
-  __device__ static void load_k(K& o, const float* k, const int64_t* off, int lane, int D) {
-    const int64_t at = off[lane & 15];
-    const float* row = k + (at < 0 ? 0 : at);
-#pragma unroll
-    for (int s = 0; s < KS; ++s) o.f[s] = chunk(row, 16 * s + 4 * (lane >> 4), D);
   }
   __device__ static void load_v(V& o, const float* v, const int64_t (&at)[NV], int lane, int D) {
 #pragma unroll
@@ -275,17 +307,19 @@ struct Tile<float, DP, PAD> {
 #pragma unroll
         for (int e = 0; e < 4; ++e) o.f[j][h][e] = at[j] < 0 ? 0.0f : o.f[j][h][e];
   }
-  __device__ static void scores(float (&s)[NV], const K& k, const Q& q) {
-    f4 acc = mma(k.f[0][0], q.f[0][0], f4{0.0f, 0.0f, 0.0f, 0.0f});
+  __device__ static void scores(float (&s)[NV], const Lds& k, const Q& q, int lane, int D) {
+    f4 acc = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-    for (int c = 0; c < KS; ++c)
+    for (int c = 0; c < KS; ++c) {
+      const f4 x = __builtin_bit_cast(f4, Rows::template operand<PAD>(k, 0, c, lane, D));
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        if (c == 0 && e == 0) continue;
-        f4 sum = mma(k.f[c][e], q.f[c][e], acc);
-        asm("" : "+v"(sum) : "v"(acc));  // nor shares part of them with the sum so far
+        f4 sum = mma(x[e], q.f[c][e], acc);
+        // nor shares part of them with the sum so far
+        if (c + e > 0) asm("" : "+v"(sum) : "v"(acc));
         acc = sum;
       }
+    }
 #pragma unroll
     for (int i = 0; i < 4; ++i) s[i] = acc[i];
   }
@@ -306,6 +340,13 @@ __device__ inline void lds_barrier() {
   __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
 }
 
+// LDS between the lanes of a wave.
+__device__ inline void wave_handoff() {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
+
 // Four values of a result row.
 template <typename T>
 __device__ inline void store4(T* p, f4 v) {
@@ -320,11 +361,11 @@ __device__ inline void store4(T* p, f4 v) {
 // may have (4 or 16; columns past them are computed on zeros).  SPLIT: a
 // workgroup takes its share of the row of tiles, otherwise one unit whole.
 //
-// The row offsets of up to kKeysAhead keys are worked out by all threads into
-// LDS (-1: masked), so that no lookup in the block table stands between the
-// loads of the loop.  The next tile's keys are loaded while this one's values
-// are used.  Every load of the loop is made, on whatever row where there is no
-// key: a wait can then count on the loads behind the one it is for.
+// The row offsets of the keys are worked out by all threads into LDS, so that no
+// lookup in the block table stands between the loads of the loop.  The next
+// tile's keys are loaded while this one's are used.  Every load of the loop is
+// made, on whatever row where there is no key: a wait can then count on the loads
+// behind the one it is for.
 template <typename T, int DP, bool PAD, int HT, int WAVES, bool SPLIT>
 __global__ __launch_bounds__(64 * WAVES, DP <= 128 ? 2 : 1) void attn_decode_kernel(AttnArgs a) {
   using M = Tile<T, DP, PAD>;
@@ -332,8 +373,12 @@ __global__ __launch_bounds__(64 * WAVES, DP <= 128 ? 2 : 1) void attn_decode_ker
     float m[WAVES][HT], l[WAVES][HT];
     __align__(16) float o[WAVES][HT][DP + 4];
   };
+  struct Loop {
+    int64_t off[3][kChunk];
+    typename M::Lds k[WAVES];
+  };
   union Lds {
-    int64_t off[kKeysAhead];
+    Loop loop;
     Join join;
   };
   __shared__ Lds lds;
@@ -388,34 +433,67 @@ __global__ __launch_bounds__(64 * WAVES, DP <= 128 ? 2 : 1) void attn_decode_ker
 #pragma unroll
       for (int i = 0; i < M::VE; ++i) o[h][i] = f4{0.0f, 0.0f, 0.0f, 0.0f};
 
-    constexpr int kTilesAhead = kKeysAhead / M::TK;
-    for (int t0 = j0; t0 < j1; t0 += kTilesAhead) {
-      const int nt = j1 - t0 < kTilesAhead ? j1 - t0 : kTilesAhead;
-      const int s0 = t0 * M::TK;
-      lds_barrier();  // what was there has been used
-      for (int i = tid; i < nt * M::TK; i += 64 * WAVES) {
-        int64_t to = -1;
-        if (s0 + i < count) {
-          const uint32_t key = (uint32_t)(first + s0 + i), c = a.page.div(key);
-          const int page = a.table[(int64_t)b * a.max_pages + c];
-          if ((uint32_t)page < (uint32_t)a.n_pages)
-            to = page * a.page_stride + (int64_t)(key - c * a.page.d) * a.token_stride;
-        }
-        lds.off[i] = to;
+    // Row offsets (-1: masked) by all threads, kChunk keys at a time: chunk c's
+    // lie at c % 3, are written a chunk before they are first used, and their
+    // block-table entries are read a chunk before that.
+    constexpr int kTiles = kChunk / M::TK, kEach = kChunk / (64 * WAVES);
+    static_assert(kTiles % WAVES == 0 && kChunk % (64 * WAVES) == 0, "whole tiles and threads");
+    const int n_tiles = j1 - j0, s0 = j0 * M::TK;
+    const int chunks = (n_tiles + kTiles - 1) / kTiles;
+    auto fetch = [&](int c, int (&page)[kEach]) {
+#pragma unroll
+      for (int e = 0; e < kEach; ++e) {
+        const uint32_t at = a.page.div(first + s0 + c * kChunk + e * 64 * WAVES + tid);
+        page[e] = a.table[(int64_t)b * a.max_pages +
+                          (at < (uint32_t)a.max_pages ? at : (uint32_t)a.max_pages - 1)];
       }
+    };
+    auto put = [&](int c, const int (&page)[kEach]) {
+#pragma unroll
+      for (int e = 0; e < kEach; ++e) {
+        const int i = e * 64 * WAVES + tid, at = s0 + c * kChunk + i;
+        const uint32_t key = (uint32_t)(first + at);
+        const bool in = at < count && (uint32_t)page[e] < (uint32_t)a.n_pages;
+        lds.loop.off[c % 3][i] =
+            in ? page[e] * a.page_stride +
+                     (int64_t)(key - a.page.div(key) * a.page.d) * a.token_stride
+               : -1;
+      }
+    };
+    int page[kEach];
+    if (n_tiles > 0) {
+      int page0[kEach];
+      fetch(0, page0);
+      if (chunks > 1) fetch(1, page);
+      lds_barrier();  // what was there has been used
+      put(0, page0);
+      if (chunks > 1) put(1, page);
       lds_barrier();
-      if (wave >= nt) continue;  // no barrier until the next offsets
-      typename M::K kf;
-      M::load_k(kf, kc, lds.off + wave * M::TK, lane, a.D);
-      for (int t = wave; t < nt; t += WAVES) {
+    }
+    typename M::K kf;
+    auto offsets = [&](int t) { return &lds.loop.off[t / kTiles % 3][t % kTiles * M::TK]; };
+    int t = wave;
+    if (t < n_tiles) M::template load<PAD>(kf, kc, offsets(t), lane, a.D);
+    for (int c = 0; c < chunks; ++c) {
+      if (c > 0) {
+        if (c + 1 < chunks) put(c + 1, page);
+        lds_barrier();  // and chunk c - 1 has been used
+      }
+      if (c + 2 < chunks) fetch(c + 2, page);
+      const int stop = n_tiles < (c + 1) * kTiles ? n_tiles : (c + 1) * kTiles;
+      for (; t < stop; t += WAVES) {
+        const int64_t* off = offsets(t);
         int64_t from[M::NV];
 #pragma unroll
-        for (int j = 0; j < M::NV; ++j) from[j] = lds.off[t * M::TK + M::key_of(j, q)];
+        for (int j = 0; j < M::NV; ++j) from[j] = off[M::key_of(j, q)];
         typename M::V vf;
         M::load_v(vf, vc, from, lane, a.D);
+        M::store(lds.loop.k[wave], kf, lane);
+        M::template load<PAD>(kf, kc, offsets(t + WAVES < n_tiles ? t + WAVES : t), lane, a.D);
+        wave_handoff();
         float s[M::NV];
-        M::scores(s, kf, qf);
-        M::load_k(kf, kc, lds.off + (t + WAVES < nt ? t + WAVES : t) * M::TK, lane, a.D);
+        M::scores(s, lds.loop.k[wave], qf, lane, a.D);
+        wave_handoff();
         bool hole = false;
         float mx = -INFINITY;
 #pragma unroll
@@ -574,19 +652,22 @@ int head_units(int B, int q_heads, int n_heads) {
 }
 
 // Workgroups of a call whose keys are split: one per CU, whose four waves keep
-// enough loads under way (64 sequences of 8192 keys, 8 heads of 128: 371 us; with
-// two 386); two where the units are many and short, so that one's start and end
-// lie under the other's loads (32 sequences of up to 2000 keys, 40 heads: 144
-// and 133 us), or the rows short (16 heads of 64: 21.6 and 20.0 us).
+// enough loads under way (1 sequence of 32768 keys, 8 heads of 128: 34.5 us, with
+// two 36.5; 64 ragged ones of up to 8192: 251 us = 5.5 TB/s, with two 260); two
+// where the units are many and short, so that one's start and end lie under the
+// other's loads (32 sequences of up to 2000 keys, 40 heads: 135 and 128 us), or the
+// rows short.  Eight waves a workgroup are as fast (249 us) or slower (4096 keys of
+// one sequence: 13.2 us, 12.7 with four).
 int split_groups(int units, int dim) {
   return kCus * (dim <= 64 || (dim <= 128 && units > 512) ? 2 : 1);
 }
 
 // Whether the keys are split.  Not where a second kernel and the look over all
-// lengths cost more than the split saves: few keys, or whole units that fill the
-// chip (64 sequences of up to 1000 keys, 8 heads of 128: whole 38.8 us, split
-// 45.0; up to 2000 keys 74 and 65 us; 4 sequences of 1000 keys 15.1 and 12.5
-// us).  Nor where a row of tiles could pass 2^31.
+// lengths cost more than the split saves: few keys (4 sequences of up to 1000 keys,
+// 8 heads of 128: whole 11.6 us, split 12.7), or whole units that fill the chip (64
+// of up to 1000: 36.7 and 44.0 us; 16 of up to 2000, 16 heads of 64: 17.4 and 19.3;
+// but 32 of up to 4096, 8 heads of 128: 70.5 and 64.1; 16 of them: 59 and 39.8).
+// Nor where a row of tiles could pass 2^31.
 bool attn_splits(int B, int q_heads, int n_heads, int keys, int64_t room) {
   if (B > kSplitSeqs) return false;
   const int64_t units = head_units(B, q_heads, n_heads);

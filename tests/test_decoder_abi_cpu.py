@@ -108,7 +108,7 @@ def test_attn_decode_refusals():
         dict(q=None), dict(o=None), dict(ln=None), dict(bt=None), dict(q=ODD), dict(o=ODD),
         dict(qs=504), dict(qs=516), dict(B=-1), dict(B=65536),
         dict(B=65535, h=128, qs=8192), dict(h=0), dict(h=6), dict(h=3),
-        dict(h=65536), dict(mp=-1), dict(ml=-1), dict(w=-1), dict(sc=float("nan")),
+        dict(h=65536), dict(mp=-1), dict(mp=(1 << 26) + 1), dict(ml=-1), dict(w=-1), dict(sc=float("nan")),
         dict(sc=float("inf"))])
     refuses("d2moe_attn_decode", ok, [dict(ws=None), dict(ws=ODD), dict(n=16)], api.EWORKSPACE)
     refuses("d2moe_attn_decode", ok, [dict(B=0)], api.OK)
