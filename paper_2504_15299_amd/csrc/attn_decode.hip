@@ -32,10 +32,9 @@ typedef uint32_t u4 __attribute__((ext_vector_type(4)));
 
 constexpr int kHeadTile = 16;    // query heads of a workgroup
 constexpr int kChunk = 512;      // keys whose row offsets are worked out at a time
-constexpr int kWholeKeys = 1024;  // up to here a workgroup takes a unit whole,
-constexpr int kManyUnits = 256;   // up to twice as many with that many units
 constexpr int kMaxSplitUnits = 2048;
 constexpr int kSplitSeqs = 256;  // most sequences of a call whose keys are split
+constexpr int kWholeBytes = 256 << 10;  // of keys: up to here a workgroup takes a unit whole
 constexpr int kMinShare = 4;     // tiles
 constexpr int kCus = 256;
 
@@ -578,11 +577,10 @@ __global__ __launch_bounds__(64 * WAVES, DP <= 128 ? 2 : 1) void attn_decode_ker
 // Joins the parts of one query head: the waves (a lane has four values) take
 // parts in turn.  A unit that one share holds whole is done already, one without
 // keys gives zeros.
-constexpr int kJoinWaves = 4;
-template <typename T, int TK>
-__global__ __launch_bounds__(64 * kJoinWaves) void attn_join_kernel(AttnArgs a) {
-  __shared__ float pm[kJoinWaves], pl[kJoinWaves];
-  __shared__ __align__(16) f4 po[kJoinWaves][64];
+template <typename T, int TK, int WAVES>
+__global__ __launch_bounds__(64 * WAVES) void attn_join_kernel(AttnArgs a) {
+  __shared__ float pm[WAVES], pl[WAVES];
+  __shared__ __align__(16) f4 po[WAVES][64];
   const int b = blockIdx.y, head = blockIdx.x;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int per = a.H * a.tiles, rows = a.G < kHeadTile ? a.G : kHeadTile;
@@ -600,12 +598,12 @@ __global__ __launch_bounds__(64 * kJoinWaves) void attn_join_kernel(AttnArgs a) 
   float mm = -INFINITY, ll = 0.0f;
   f4 acc = {0.0f, 0.0f, 0.0f, 0.0f};
   constexpr int kAhead = 4;  // parts loaded together
-  for (int i = wave; i < n; i += kAhead * kJoinWaves) {
+  for (int i = wave; i < n; i += kAhead * WAVES) {
     float2 ml[kAhead];
     f4 v[kAhead];
 #pragma unroll
     for (int k = 0; k < kAhead; ++k) {
-      const int64_t p = part(i + k * kJoinWaves < n ? i + k * kJoinWaves : i);
+      const int64_t p = part(i + k * WAVES < n ? i + k * WAVES : i);
       ml[k] = *(const float2*)(a.part_ml + p * 2);
       v[k] = *(const f4*)(a.part_o + p * a.D + d);
     }
@@ -618,7 +616,7 @@ __global__ __launch_bounds__(64 * kJoinWaves) void attn_join_kernel(AttnArgs a) 
     acc *= alpha;
 #pragma unroll
     for (int k = 0; k < kAhead; ++k) {
-      if (i + k * kJoinWaves >= n) break;
+      if (i + k * WAVES >= n) break;
       const float f = fast_exp2(ml[k].x - ref);
       ll = fmaf(f, ml[k].y, ll);
       acc += f * v[k];
@@ -629,12 +627,12 @@ __global__ __launch_bounds__(64 * kJoinWaves) void attn_join_kernel(AttnArgs a) 
   __syncthreads();
   if (wave != 0 || 4 * lane >= a.D) return;
 #pragma unroll
-  for (int w = 1; w < kJoinWaves; ++w) mm = fmaxf(mm, pm[w]);
+  for (int w = 1; w < WAVES; ++w) mm = fmaxf(mm, pm[w]);
   const float ref = mm == -INFINITY ? 0.0f : mm;
   ll = 0.0f;
   acc = f4{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-  for (int w = 0; w < kJoinWaves; ++w) {
+  for (int w = 0; w < WAVES; ++w) {
     const float f = fast_exp2(pm[w] - ref);
     ll = fmaf(f, pl[w], ll);
     acc += f * po[w][lane];
@@ -662,16 +660,21 @@ int split_groups(int units, int dim) {
   return kCus * (dim <= 64 || (dim <= 128 && units > 512) ? 2 : 1);
 }
 
-// Whether the keys are split.  Not where a second kernel and the look over all
-// lengths cost more than the split saves: few keys (4 sequences of up to 1000 keys,
-// 8 heads of 128: whole 11.6 us, split 12.7), or whole units that fill the chip (64
-// of up to 1000: 36.7 and 44.0 us; 16 of up to 2000, 16 heads of 64: 17.4 and 19.3;
-// but 32 of up to 4096, 8 heads of 128: 70.5 and 64.1; 16 of them: 59 and 39.8).
-// Nor where a row of tiles could pass 2^31.
-bool attn_splits(int B, int q_heads, int n_heads, int keys, int64_t room) {
+// Whether the keys are split.  Not where a second kernel, the look over all lengths
+// and a cold start of every share cost more than the split saves: up to 256 KB of keys
+// a unit (16 sequences of up to 1000 keys, 8 heads of 128, bf16: whole 13.6 us, split
+// 18.9, up to 2000: 18.8 and 21; 16 of 2000, 64 a head: 16.0 and 20.7, up to 3000: 20.8
+// and 20.2; fp32, 16 of up to 1000, 64 a head: both 16.7, up to 1500: 23.3 and 18.8),
+// twice that in bf16 where the units fill the chip by themselves (64 of up to 1500,
+// 8 heads of 128: 47.2 and 56.1, but 32 of up to 4096: 70.5 and 64.1; fp32, whose units
+// take longer: 64 of up to 2000, 12 heads of 64: 94.5 and 79.3).  Nor where a row of
+// tiles could pass 2^31.
+bool attn_splits(int B, int q_heads, int n_heads, int dim, int size, int keys, int64_t room) {
   if (B > kSplitSeqs) return false;
   const int64_t units = head_units(B, q_heads, n_heads);
-  return keys > (units < kManyUnits ? kWholeKeys : 2 * kWholeKeys) && units < kMaxSplitUnits &&
+  const int64_t unit_bytes = (int64_t)keys * size * (dim <= 64 ? 64 : dim <= 128 ? 128 : 256);
+  return unit_bytes > (size == 2 && units > kCus ? 2 : 1) * kWholeBytes &&
+         units < kMaxSplitUnits &&
          units * ((room < 0x7fffffff ? room : 0x7fffffff) / 16 + 1) < 0x7fffffff;
 }
 
@@ -694,8 +697,14 @@ hipError_t run_attn(const AttnArgs& a, bool split, hipStream_t s) {
     run_attn_h<T, DP, PAD, 16>(a, split, s);
   const hipError_t err = hipGetLastError();
   if (err != hipSuccess || !split) return err;
-  attn_join_kernel<T, Tile<T, DP, PAD>::TK>
-      <<<dim3(a.Hq, a.B), 64 * kJoinWaves, 0, s>>>(a);
+  constexpr int TK = Tile<T, DP, PAD>::TK;
+  // 16 waves for many parts a unit (100000 keys of one key head: 22.4 us for both
+  // kernels, with four waves 36.9; 32 parts: 11.8 and 12.8), four for few (16 sequences
+  // of up to 4096 keys, 8 heads of 128: 39.7 us, with sixteen 41.0)
+  if (a.groups >= 16 * a.B * a.H * a.tiles)
+    attn_join_kernel<T, TK, 16><<<dim3(a.Hq, a.B), 1024, 0, s>>>(a);
+  else
+    attn_join_kernel<T, TK, 4><<<dim3(a.Hq, a.B), 256, 0, s>>>(a);
   return hipGetLastError();
 }
 
@@ -712,7 +721,8 @@ hipError_t run_attn_t(const AttnArgs& a, bool split, hipStream_t s) {
 }  // namespace
 
 size_t attn_decode_workspace(int B, int q_heads, int n_heads, int dim, int max_len) {
-  if (B == 0 || !attn_splits(B, q_heads, n_heads, max_len, 0)) return 0;
+  // (fp32 caches, the first to be split)
+  if (B == 0 || !attn_splits(B, q_heads, n_heads, dim, 4, max_len, 0)) return 0;
   const int rows = q_heads / n_heads < kHeadTile ? q_heads / n_heads : kHeadTile;
   return (size_t)split_groups(head_units(B, q_heads, n_heads), dim) * 2 * rows * (dim + 2) *
          sizeof(float);
@@ -731,8 +741,8 @@ hipError_t launch_attn_decode(const void* q, int64_t q_stride, int B, int q_head
   a.G = q_heads / c->n_heads, a.tiles = head_tiles(q_heads, c->n_heads), a.D = c->head_dim;
   a.window = window;
   const int keys = window > 0 && window < max_len ? window : max_len;
-  const bool split =
-      attn_splits(B, q_heads, c->n_heads, keys, (int64_t)max_pages * c->page_size);
+  const bool split = attn_splits(B, q_heads, c->n_heads, a.D, c->dtype == D2MOE_BF16 ? 2 : 4, keys,
+                                 (int64_t)max_pages * c->page_size);
   a.groups = split_groups(head_units(B, q_heads, c->n_heads), a.D);
   a.scale_log2 = scale * 1.44269504088896340736f;
   a.out = out;
