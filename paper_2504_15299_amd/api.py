@@ -427,10 +427,14 @@ def _arg(t, shape, dtype, dev, what):
 
 
 def _new(like, shape, dtype, stream):
-    """A tensor for a call on ``stream`` (None: the current one)."""
-    t = like.new_empty(shape, dtype=dtype)
-    if stream is not None:
-        t.record_stream(stream)
+    """A tensor for a call on ``stream`` (None: the current one): memory that
+    the current stream has freed may still be in use there, so it is taken from
+    ``stream``'s own, and kept until the current one is past its uses."""
+    if stream is None:
+        return like.new_empty(shape, dtype=dtype)
+    with torch.cuda.stream(stream):
+        t = like.new_empty(shape, dtype=dtype)
+    t.record_stream(torch.cuda.current_stream(like.device))
     return t
 
 
