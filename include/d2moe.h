@@ -536,7 +536,7 @@ typedef struct {
  * sequence is outside [0, n_seqs) or whose page is outside [0, n_pages) is
  * not written to the cache; its q row goes to q_out unrotated when its
  * position is outside [0, n_rot), rotated otherwise.  No two tokens of a call
- * may share a place in the cache.
+ * may share a place in the cache.  N <= 2^30, q_heads and n_heads <= 65536.
  */
 d2moe_status d2moe_kv_append(const void* q, int64_t q_stride, int32_t q_heads, const void* k,
                              const void* v, int64_t kv_stride, d2moe_dtype x_dtype, int32_t N,

@@ -360,7 +360,8 @@ d2moe_status d2moe_kv_append(const void* q, int64_t q_stride, int32_t q_heads, c
                              const int32_t* token_seq, const float* cos, const float* sin,
                              int32_t n_rot, void* q_out, void* stream) {
   if (!dtype_ok(x_dtype)) return D2MOE_EUNSUPPORTED;
-  if (N < 0 || !cache_ok(cache) || n_seqs < 0 || max_pages < 0) return D2MOE_EINVAL;
+  if (N < 0 || N > (1 << 30) || !cache_ok(cache) || n_seqs < 0 || max_pages < 0)
+    return D2MOE_EINVAL;
   if (!cos != !sin || (cos && (n_rot < 0 || !aligned(cos, 16) || !aligned(sin, 16))))
     return D2MOE_EINVAL;
   if (N == 0) return D2MOE_OK;

@@ -90,8 +90,8 @@ def test_kv_append_refusals():
               p=FAKE, sq=None, co=FAKE, si=FAKE, nr=100, qo=2 * FAKE, s=None)
     refuses("d2moe_kv_append", ok, [dict(c=cache(**b)) for b in BAD_CACHES])
     refuses("d2moe_kv_append", ok, [
-        dict(N=-1), dict(ns=-1), dict(mp=-1), dict(k=None), dict(v=None), dict(p=None),
-        dict(bt=None), dict(qo=None), dict(co=None), dict(si=None), dict(nr=-1), dict(h=0),
+        dict(N=-1), dict(N=(1 << 30) + 1), dict(ns=-1), dict(mp=-1), dict(k=None), dict(v=None),
+        dict(p=None), dict(bt=None), dict(qo=None), dict(co=None), dict(si=None), dict(nr=-1), dict(h=0),
         dict(h=70000), dict(q=ODD), dict(k=ODD), dict(v=ODD), dict(qo=2 * FAKE + 8),
         dict(co=FAKE + 4), dict(si=FAKE + 4), dict(qs=504), dict(qs=516), dict(ks=248),
         dict(ks=260),
