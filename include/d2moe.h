@@ -484,9 +484,11 @@ d2moe_status d2moe_linear_pack_codes(const uint8_t* codes, const uint16_t* scale
  *   y:    device [T][rows] (y_dtype); bf16 is rounded to nearest even
  * Products are exact and summed in binary32 within a group, groups in
  * binary32.  A token with an infinity or NaN among its activations gets NaN or
- * infinite results; other tokens' do not depend on it.  Any T >= 0; made for
- * the T of a decode step: above 64 tokens the weights are read again for
- * every 64.  No workspace; results do not depend on what else runs.
+ * infinite results; other tokens' do not depend on it.  0 <= T <= 2^20; made
+ * for the T of a decode step: above 64 tokens the weights are read again for
+ * every 64.  The sums are of (16 + n) x, which a group's activations must keep
+ * within binary32.  y does not overlap x.  No workspace; results do not depend
+ * on what else runs.
  */
 d2moe_status d2moe_linear_forward(const void* x, d2moe_dtype x_dtype, int32_t T,
                                   const d2moe_linear* w, const float* bias, void* y,
@@ -554,7 +556,8 @@ d2moe_status d2moe_kv_append(const void* q, int64_t q_stride, int32_t q_heads, c
  *   q:   device [B][q_heads][head_dim] of the cache's type, sequences
  *        q_stride elements apart, 16-byte aligned
  *   block_table: device [B][max_pages] int32; lengths: device [B] int32
- *   out: device [B][q_heads][head_dim] of the cache's type
+ *   out: device [B][q_heads][head_dim] of the cache's type; may be q when q
+ *        is packed
  *   max_len: host, the largest length expected; only the division of the work
  *        goes by it, any length gives its result
  *   workspace: at least d2moe_attn_decode_workspace bytes for this max_len or
@@ -564,7 +567,8 @@ d2moe_status d2moe_kv_append(const void* q, int64_t q_stride, int32_t q_heads, c
  * page_size <= 2^30; scale is finite.  A sequence of length 0
  * (or less) gives zeros; a length beyond the table's row counts as the row's
  * end; a token whose page is outside [0, n_pages) counts as masked, and a row
- * with every token masked gives zeros.  Cache rows outside the tokens
+ * with every token masked gives zeros.  So does a row whose scores are all
+ * -infinity.  Cache rows outside the tokens
  * attended are not used, whatever they hold.  Scores, softmax and sums are
  * binary32; with a bf16 cache the probabilities enter the value product as
  * two bf16 terms.
@@ -589,7 +593,7 @@ d2moe_status d2moe_attn_decode(const void* q, int64_t q_stride, int32_t B, int32
  *   gate: device (gate_dtype), token t's row gate_stride * t elements from
  *        the start (gate_stride 0: one row for all tokens), or NULL (ones)
  *   h: device [T][d] (h_dtype; bf16 is rounded to nearest even), or NULL
- *        (only x is updated)
+ *        (only x is updated); may be y when of y's type
  * 1 <= d <= 16384, T >= 0, eps >= 0, gate_stride 0 or >= d.  Accumulation is
  * fp32.
  */

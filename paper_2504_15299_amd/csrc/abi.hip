@@ -39,8 +39,8 @@ bool dtype_ok(d2moe_dtype t) { return t == D2MOE_F32 || t == D2MOE_BF16; }
 int64_t dtype_size(d2moe_dtype t) { return t == D2MOE_BF16 ? 2 : 4; }
 
 bool linear_shape_ok(int rows, int cols, int group) {
-  return rows >= 1 && (group == 32 || group == 64 || group == 128) && cols >= group &&
-         cols % group == 0 && cols <= (1 << 22);
+  return rows >= 1 && rows <= (1 << 27) && (group == 32 || group == 64 || group == 128) &&
+         cols >= group && cols % group == 0 && cols <= (1 << 22);
 }
 
 bool linear_ok(const d2moe_linear* w) {

@@ -19,6 +19,7 @@ struct NormArgs {
   int64_t gate_stride;
   float x_scale, y_scale, eps;
   int d;
+  int64_t row0;  // of this launch
   bool y_bf, g_bf, h_bf;
 };
 
@@ -114,8 +115,8 @@ __device__ inline float group_sum(float v, float* part) {
 template <int THREADS, int NPER, bool AHEAD, bool PAST>
 __global__ __launch_bounds__(THREADS) void block_norm_kernel(NormArgs a) {
   __shared__ float part[2][THREADS / 64];
-  const int64_t row = (int64_t)blockIdx.x * a.d;
-  const int64_t grow = (int64_t)blockIdx.x * a.gate_stride;
+  const int64_t row = (a.row0 + blockIdx.x) * a.d;
+  const int64_t grow = (a.row0 + blockIdx.x) * a.gate_stride;
   float x[NPER][4], u[NPER][4], g[NPER][4], post[NPER][4], pre[NPER][4];
   auto load_rest = [&](int i, int c, int n) {
     if (a.post_w) load_row(a.post_w, false, c, n, post[i]);
@@ -179,7 +180,11 @@ __global__ __launch_bounds__(THREADS) void block_norm_kernel(NormArgs a) {
 
 template <int THREADS, int NPER, bool AHEAD, bool PAST>
 void run_block_norm_n(const NormArgs& a, int T, hipStream_t s) {
-  block_norm_kernel<THREADS, NPER, AHEAD, PAST><<<T, THREADS, 0, s>>>(a);
+  // a grid has fewer than 2^32 threads
+  constexpr int kRows = 1 << 21;
+  for (NormArgs b = a; b.row0 < T; b.row0 += kRows)
+    block_norm_kernel<THREADS, NPER, AHEAD, PAST>
+        <<<T - b.row0 < kRows ? T - b.row0 : kRows, THREADS, 0, s>>>(b);
 }
 
 // Threads a row, by its runs of four values: one run a thread leaves the shortest

@@ -27,7 +27,7 @@ def linear(**kw):
     return api._Linear(**d)
 
 
-BAD_LINEARS = [dict(rows=0), dict(rows=-16), dict(cols=0), dict(cols=-256), dict(cols=200),
+BAD_LINEARS = [dict(rows=0), dict(rows=(1 << 27) + 1), dict(rows=-16), dict(cols=0), dict(cols=-256), dict(cols=200),
                dict(cols=32), dict(group=16), dict(group=0), dict(group=256), dict(codes=0),
                dict(scales=0), dict(zeros=0), dict(codes=ODD), dict(cols=(1 << 22) + 64)]
 

@@ -52,3 +52,69 @@ def test_result_on_another_stream_does_not_take_memory_in_use(name):
     out = run()
     torch.cuda.synchronize()
     assert out.numel() == 512 and (kept == 7.0).all()
+
+
+def test_linear_of_the_most_tokens():
+    """2^20 tokens, which every division of the work has to reach with its grid."""
+    T = 1 << 20
+    x = torch.randn((T, 128), device=DEV).to(BF)
+    for group in (32, 128):
+        w = api.linear_pack(torch.randn((16, 128), device=DEV), api.Linear.empty(16, 128, group, DEV))
+        y = api.linear_forward(x, w)
+        for t in (0, 12345, T - 20):
+            assert torch.equal(y[t:t + 20], api.linear_forward(x[t:t + 20].contiguous(), w))
+
+
+def test_norm_of_more_rows_than_a_grid_has():
+    """A row of one value: h = x / |x|, x = x + y exact here."""
+    T = (1 << 26) + 5
+    x = (torch.arange(T, dtype=I32, device=DEV) % 31 - 15).to(F32)[:, None]
+    y = torch.full((T, 1), 0.5, dtype=BF, device=DEV)
+    want = x + 0.5
+    h = api.block_norm(x, y, eps=0.0)
+    assert torch.equal(x, want)
+    assert torch.equal(h.float(), want.sign())
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("max_len", [100, 5000])
+def test_attention_over_its_queries(dtype, max_len):
+    cache = cache_of(300, 16, 2, 128, dtype)
+    table = torch.randperm(300, device=DEV).to(I32)[:300].view(3, 100)
+    lengths = torch.tensor([1500, 40, 700], dtype=I32, device=DEV)
+    q = torch.randn((3, 36, 128), device=DEV).to(dtype)
+    want = api.attn_decode(q, cache, table, lengths, max_len=max_len)
+    assert torch.equal(api.attn_decode(q, cache, table, lengths, max_len=max_len, out=q), want)
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("d", [7, 4096, 16384])
+def test_norm_over_its_addend(d, dtype):
+    x, y = torch.randn((300, d), device=DEV), torch.randn((300, d), device=DEV).to(dtype)
+    w, x2 = torch.rand(d, device=DEV), x.clone()
+    want = api.block_norm(x2, y, post_weight=w, pre_weight=w, h_dtype=dtype)
+    h = api.block_norm(x, y, post_weight=w, pre_weight=w, h=y)
+    assert torch.equal(x, x2) and torch.equal(h, want)
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+def test_attention_of_one_head_over_many_parts(dtype):
+    """A key head whose keys are divided over all workgroups, joined again, against
+    the same keys as 40 sequences by their sums in binary64."""
+    n, D = 40000, 64
+    cache = cache_of(n // 16, 16, 1, D, dtype)
+    table = torch.randperm(n // 16, device=DEV).to(I32)[None]
+    q = torch.randn((1, 5, D), device=DEV).to(dtype)
+    got = api.attn_decode(q, cache, table, torch.tensor([n - 3], dtype=I32, device=DEV))
+    k, v = (t[table[0].long()].reshape(n, D)[:n - 3].double().cpu() for t in (cache.k, cache.v))
+    s = (q[0].double().cpu() @ k.t()) * D ** -0.5
+    p = torch.softmax(s, 1)
+    want = p @ v
+    # scores of 64 products in binary32: off by 64 2^-24 of the sum of |products|,
+    # which is at most |q| |k|; a probability by twice that, a value sum by 2^-16 of
+    # the sum of p |v| (two bf16 terms) and by 40000 2^-24 at most in binary32
+    ds = 64 * 2.0 ** -24 * (q[0].double().cpu().norm(dim=1, keepdim=True) * k.norm(dim=1)).max() / 8
+    mag = p @ v.abs()
+    err = mag * (2 * ds + 2.0 ** -16 + n * 2.0 ** -24) + \
+        want.abs() * torch.finfo(dtype).eps / 2 + 1e-30
+    assert ((got[0].double().cpu() - want).abs() <= err).all()
