@@ -419,18 +419,23 @@ def residual_rmsnorm(x: torch.Tensor, y: torch.Tensor | None, eps: float = 1e-5,
 
 # ---- the rest of a decoder block: 4-bit linear layers, paged cache, norms ------
 
+# Tensors' devices are compared by their index (-1 for the CPU), which costs half
+# of what comparing device objects does.
+
 def _arg(t, shape, dtype, dev, what):
     """Pointer of a contiguous tensor of this shape and type."""
-    if t.dtype != dtype or t.shape != shape or t.device != dev or not t.is_contiguous():
-        raise ValueError(f"{what} must be a contiguous {dtype} tensor of shape {shape} on {dev}")
+    if t.dtype != dtype or t.shape != shape or t.get_device() != dev or not t.is_contiguous():
+        raise ValueError(f"{what} must be a contiguous {dtype} tensor of shape {shape} on GPU {dev}")
     return t.data_ptr()
 
 
 def _new(like, shape, dtype, stream):
-    """A tensor for a call on ``stream`` (None: the current one): memory that
+    """A contiguous tensor for a call on ``stream`` (None: the current one): memory that
     the current stream has freed may still be in use there, so it is taken from
     ``stream``'s own, and kept until the current one is past its uses."""
     if stream is None:
+        if like.shape == shape and like.dtype == dtype and like.is_contiguous():
+            return torch.empty_like(like)  # the same, sooner
         return like.new_empty(shape, dtype=dtype)
     with torch.cuda.stream(stream):
         t = like.new_empty(shape, dtype=dtype)
@@ -444,18 +449,17 @@ _entry = {}     # entry points by name
 
 def _run(name, dev, stream, *args):
     """The entry point on ``stream`` (None: the current one of the tensors'
-    device), with that device current."""
+    device, number ``dev``), with that device current."""
     fn = _entry.get(name)
     if fn is None:
         fn = _entry[name] = getattr(lib(), name)
-    index = dev.index
-    if dev.type != "cuda" or index is None:
-        raise ValueError(f"{name}: tensors must be on a GPU, not on {dev}")
-    raw = torch._C._cuda_getCurrentRawStream(index) if stream is None else stream.cuda_stream
-    if index == torch._C._cuda_getDevice():
+    if dev < 0:
+        raise ValueError(f"{name}: tensors must be on a GPU")
+    raw = torch._C._cuda_getCurrentRawStream(dev) if stream is None else stream.cuda_stream
+    if dev == torch._C._cuda_getDevice():
         rc = fn(*args, raw)
     else:
-        with torch.cuda.device(index):
+        with torch.cuda.device(dev):
             rc = fn(*args, raw)
     if rc != OK:
         raise D2MoEError(name, rc)
@@ -478,7 +482,7 @@ class Linear:
                     t.device != codes.device:
                 raise ValueError(f"buffers of {sizes} bytes on one device are needed")
         self.rows, self.cols, self.group = rows, cols, group
-        self.codes, self.scales, self.zeros = codes, scales, zeros
+        self.codes, self.scales, self.zeros, self.index = codes, scales, zeros, codes.get_device()
         self._c = _Linear(rows, cols, group, codes.data_ptr(), scales.data_ptr(),
                           zeros.data_ptr())
         self._ref = ctypes.byref(self._c)
@@ -496,7 +500,7 @@ class Linear:
 
 def linear_pack(W: torch.Tensor, out: Linear, stream=None) -> Linear:
     """``d2moe_linear_pack``: quantize + pack W [rows][cols] (fp32, device)."""
-    dev = out.codes.device
+    dev = out.index
     _run("d2moe_linear_pack", dev, stream,
          _arg(W, (out.rows, out.cols), torch.float32, dev, "W"), D2MOE_F32, out._ref)
     return out
@@ -506,7 +510,7 @@ def linear_pack_codes(codes: torch.Tensor, scales: torch.Tensor, zeros, out: Lin
                       stream=None) -> Linear:
     """``d2moe_linear_pack_codes``: codes [rows][cols] uint8 (0..15), scales
     [rows][cols/group] float16, zeros [rows][cols/group] uint8 or None (8)."""
-    dev, g = out.codes.device, (out.rows, out.cols // out.group)
+    dev, g = out.index, (out.rows, out.cols // out.group)
     _run("d2moe_linear_pack_codes", dev, stream,
          _arg(codes, (out.rows, out.cols), torch.uint8, dev, "codes"),
          _arg(scales, g, torch.float16, dev, "scales"),
@@ -518,7 +522,7 @@ def linear_forward(x: torch.Tensor, w: Linear, bias: torch.Tensor | None = None,
                    y: torch.Tensor | None = None, y_dtype=None, stream=None) -> torch.Tensor:
     """``d2moe_linear_forward``: x [T][cols] -> [T][rows] (y_dtype, x's type
     when not given); bias [rows] float32 or None."""
-    T, dev, dtype = x.shape[0], w.codes.device, x.dtype
+    T, dev, dtype = x.shape[0], w.index, x.dtype
     px = _arg(x, (T, w.cols), dtype, dev, "x")
     if y is None:
         y = _new(x, (T, w.rows), y_dtype or dtype, stream)
@@ -545,6 +549,7 @@ class KVCache:
                              "and stride, dim contiguous")
         self.k, self.v = k, v
         self.n_pages, self.page_size, self.n_heads, self.head_dim = k.shape
+        self.index = k.get_device()
         self._c = _KVCache(*k.shape, _dtype_code(k), *k.stride()[:3], k.data_ptr(), v.data_ptr())
         self._ref = ctypes.byref(self._c)
 
@@ -558,8 +563,8 @@ class KVCache:
 def _rows(t, shape, dtype, dev, what):
     """Pointer and token stride of a [token][head][dim] tensor whose heads are
     packed."""
-    if t.shape != shape or t.dtype != dtype or t.device != dev:
-        raise ValueError(f"{what} must be a {dtype} tensor of shape {shape} on {dev}")
+    if t.shape != shape or t.dtype != dtype or t.get_device() != dev:
+        raise ValueError(f"{what} must be a {dtype} tensor of shape {shape} on GPU {dev}")
     n, heads, dim = shape
     row, head, one = t.stride()
     if one != 1 or (heads > 1 and head != dim):
@@ -575,7 +580,7 @@ def kv_append(q, k: torch.Tensor, v: torch.Tensor, cache: KVCache, block_table: 
     [n_seqs][max_pages], positions [N] and token_seq [N] int32, cos and sin
     [n_rot][dim/2] float32.  Returns q_out [N][q_heads][dim] of the cache's
     type (None without q)."""
-    dev, dtype, N, D = cache.k.device, k.dtype, k.shape[0], cache.head_dim
+    dev, dtype, N, D = cache.index, k.dtype, k.shape[0], cache.head_dim
     shape = (N, cache.n_heads, D)
     pk, ks = _rows(k, shape, dtype, dev, "k")
     pv, vs = _rows(v, shape, dtype, dev, "v")
@@ -588,7 +593,7 @@ def kv_append(q, k: torch.Tensor, v: torch.Tensor, cache: KVCache, block_table: 
         heads = q.shape[1]
         pq, qs = _rows(q, (N, heads, D), dtype, dev, "q")
         if q_out is None:
-            q_out = _new(k, (N, heads, D), cache.k.dtype, stream)
+            q_out = _new(q, (N, heads, D), cache.k.dtype, stream)
             po = q_out.data_ptr()
         else:
             po = _arg(q_out, (N, heads, D), cache.k.dtype, dev, "q_out")
@@ -620,7 +625,7 @@ def attn_decode(q: torch.Tensor, cache: KVCache, block_table: torch.Tensor, leng
     block_table [B][max_pages] and lengths [B] int32 (device) -> out
     [B][q_heads][dim].  ``scale`` is 1 / sqrt(dim) when not given, ``max_len``
     the length that fills a row of the table."""
-    dev, dtype, D = cache.k.device, cache.k.dtype, cache.head_dim
+    dev, dtype, D = cache.index, cache.k.dtype, cache.head_dim
     B, heads = q.shape[:2]
     shape = (B, heads, D)
     pq, qs = _rows(q, shape, dtype, dev, "q")
@@ -636,8 +641,8 @@ def attn_decode(q: torch.Tensor, cache: KVCache, block_table: torch.Tensor, leng
         need = attn_decode_workspace(B, heads, cache, max_len)
         if need:
             workspace = _new(q, (need,), torch.uint8, stream)
-    elif workspace.device != dev or not workspace.is_contiguous():
-        raise ValueError(f"workspace must be a contiguous tensor on {dev}")
+    elif workspace.get_device() != dev or not workspace.is_contiguous():
+        raise ValueError(f"workspace must be a contiguous tensor on GPU {dev}")
     pw, nw = (None, 0) if workspace is None else (workspace.data_ptr(), workspace.nbytes)
     _run("d2moe_attn_decode", dev, stream, pq, qs, B, heads, cache._ref,
          _arg(block_table, (B, pages), torch.int32, dev, "block_table"), pages,
@@ -653,22 +658,22 @@ def block_norm(x: torch.Tensor, y: torch.Tensor, eps: float = 1e-5, pre_weight=N
     x_scale * x + y_scale * gate * postnorm(y); returns h = prenorm(x) (h_dtype;
     None: only x is updated).  y [T][d]; gate [d] or [T][d] (rows may be
     strided); pre_weight, post_weight [d] float32 or None."""
-    shape, dev, f32 = x.shape, x.device, torch.float32
+    shape, dev, f32 = x.shape, x.get_device(), torch.float32
     T, d = shape
     px, py = _arg(x, shape, f32, dev, "x"), _arg(y, shape, y.dtype, dev, "y")
     pg, gs, gd = None, 0, D2MOE_F32
     if gate is not None:
         rows = gate.dim() == 2
-        if gate.shape != (shape if rows else (d,)) or gate.device != dev or \
+        if gate.shape != (shape if rows else (d,)) or gate.get_device() != dev or \
                 (d > 1 and gate.stride(-1) != 1):
-            raise ValueError(f"gate must be [d] or [T][d] = {(T, d)} on {dev}, rows contiguous")
+            raise ValueError(f"gate must be [d] or [T][d] = {(T, d)} on GPU {dev}, rows contiguous")
         # one row alone has no stride
         pg, gs, gd = gate.data_ptr(), gate.stride(0) if rows and T > 1 else 0, _dtype_code(gate)
     ph, hd = None, D2MOE_F32
     if h is not None:
         ph, hd = _arg(h, shape, h.dtype, dev, "h"), _dtype_code(h)
     elif h_dtype is not None:
-        h = _new(x, shape, h_dtype, stream)
+        h = _new(y, shape, h_dtype, stream)
         ph, hd = h.data_ptr(), _dtype_code(h)
     _run("d2moe_block_norm", dev, stream, px, x_scale, py, _dtype_code(y), y_scale,
          None if post_weight is None else _arg(post_weight, (d,), f32, dev, "post_weight"), pg, gd,
