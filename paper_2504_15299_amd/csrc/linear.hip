@@ -22,6 +22,9 @@ typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef __bf16 b2 __attribute__((ext_vector_type(2)));
 typedef float f4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u4 __attribute__((ext_vector_type(4)));
+// four results of a token, whose row starts at any element
+typedef float row4 __attribute__((ext_vector_type(4), aligned(4)));
+typedef uint16_t row4h __attribute__((ext_vector_type(4), aligned(2)));
 
 struct LinArgs {
   const void* x;
@@ -120,6 +123,13 @@ __device__ inline void lds_barrier() {
   __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
   __builtin_amdgcn_s_barrier();
   __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
+}
+
+__device__ inline void put(const LinArgs& a, int64_t at, float v) {
+  if (a.y_bf)
+    ((uint16_t*)a.y)[at] = f2bf(v);
+  else
+    ((float*)a.y)[at] = v;
 }
 
 // What a lane needs of one column block for RT row tiles, beside x.
@@ -258,6 +268,8 @@ __global__ __launch_bounds__(64 * R * S) void linear_kernel(LinArgs a) {
           xp[j & 1][n][k] = lds.st.x[buf][sk][k][(n * 4 + j) * 64 + q * 16 + (col ^ (4 * j + q))];
     };
     read_x(0);
+    store_x(x, buf ^ 1);  // under the first operands' way from LDS
+    load_x(x, (it + 3) * S + sk);
 #pragma unroll
     for (int g = 0; g < GB; ++g) {
       f4 acc[RT][NT][NA];
@@ -304,8 +316,6 @@ __global__ __launch_bounds__(64 * R * S) void linear_kernel(LinArgs a) {
       }
     }
     load_w(w, a, rb0, (it + 2) * S + sk, lane);
-    store_x(x, buf ^ 1);
-    load_x(x, (it + 3) * S + sk);
     hand_over();
   };
   WFrag<RT, GB> w0, w1;
@@ -323,27 +333,51 @@ __global__ __launch_bounds__(64 * R * S) void linear_kernel(LinArgs a) {
     step(it + 1, std::integral_constant<int, 1>{}, w1, x0);
   }
   lds_barrier();  // the buffers become the waves' results
+  // A lane's four rows (16 r + 4 q .. + 3 of token 16 n + col) stay together; 8
+  // threads that take the quads of one token after the other meet 8 different bank
+  // groups.
+  auto place = [](int tile, int quad, int t) { return quad * 16 + (t ^ (quad | (tile & 1) << 2)); };
 #pragma unroll
   for (int r = 0; r < RT; ++r)
 #pragma unroll
     for (int n = 0; n < NT; ++n)
-      lds.part[sk][rw * RT + r][n][lane] = f4{y[r][n][0], y[r][n][1], y[r][n][2], y[r][n][3]};
+      lds.part[sk][rw * RT + r][n][place(rw * RT + r, q, col)] =
+          f4{y[r][n][0], y[r][n][1], y[r][n][2], y[r][n][3]};
   lds_barrier();
-  // row 16 r + i of token 16 n + t lies in tile (r, n), lane 16 (i / 4) + t, i % 4
-  constexpr int kRows = 16 * R * RT;
-  for (int o = threadIdx.x; o < kRows * 16 * NT; o += 64 * R * S) {
-    const int i = o % kRows, t = o / kRows, row = blockIdx.x * kRows + i;
-    if (row >= a.rows || t0 + t >= a.T) continue;
-    float sum = 0.0f;
+  constexpr int kQuads = 4 * R * RT;
+  if constexpr (NT * RT >= S) {
+    // a quad a thread, where that leaves no thread idle (32000 x 4096 at 64 tokens: 32.8
+    // us with a value a thread, 31.8 so; one token of 4096 x 4096: 4.24 and 4.48)
+    for (int o = threadIdx.x; o < kQuads * 16 * NT; o += 64 * R * S) {
+      const int i = o % kQuads, t = o / kQuads, row = (blockIdx.x * kQuads + i) * 4;
+      if (row >= a.rows || t0 + t >= a.T) continue;
+      f4 sum = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-    for (int w = 0; w < S; ++w)
-      sum += lds.part[w][i >> 4][t >> 4][((i & 15) >> 2) * 16 + (t & 15)][i & 3];
-    if (a.bias) sum += a.bias[row];
-    const int64_t to = (int64_t)(t0 + t) * a.rows + row;
-    if (a.y_bf)
-      ((uint16_t*)a.y)[to] = f2bf(sum);
-    else
-      ((float*)a.y)[to] = sum;
+      for (int w = 0; w < S; ++w) sum += lds.part[w][i >> 2][t >> 4][place(i >> 2, i & 3, t & 15)];
+      const int64_t to = (int64_t)(t0 + t) * a.rows + row;
+      if (row + 4 <= a.rows) {
+        if (a.bias) sum += *(const row4*)(a.bias + row);
+        if (a.y_bf)
+          *(row4h*)((uint16_t*)a.y + to) =
+              row4h{f2bf(sum[0]), f2bf(sum[1]), f2bf(sum[2]), f2bf(sum[3])};
+        else
+          *(row4*)((float*)a.y + to) = sum;
+      } else {
+#pragma unroll
+        for (int e = 0; e < 3; ++e)
+          if (row + e < a.rows) put(a, to + e, sum[e] + (a.bias ? a.bias[row + e] : 0.0f));
+      }
+    }
+  } else {
+    for (int o = threadIdx.x; o < kQuads * 64 * NT; o += 64 * R * S) {
+      const int i = o % (4 * kQuads), t = o / (4 * kQuads), row = blockIdx.x * 4 * kQuads + i;
+      if (row >= a.rows || t0 + t >= a.T) continue;
+      float sum = 0.0f;
+#pragma unroll
+      for (int w = 0; w < S; ++w)
+        sum += lds.part[w][i >> 4][t >> 4][place(i >> 4, i >> 2 & 3, t & 15)][i & 3];
+      put(a, (int64_t)(t0 + t) * a.rows + row, sum + (a.bias ? a.bias[row] : 0.0f));
+    }
   }
 }
 
@@ -361,25 +395,26 @@ hipError_t run_linear_g(const LinArgs& a, hipStream_t s) {
 // the activations (whose reading from L2 bounds the kernel otherwise) while one
 // round of workgroups fills the chip.  Measured, bf16, 4096 columns, group 128, us:
 //   R, S of 16-token workgroups         1, 8   2, 4   4, 4   8, 2
-//   4096 rows x 16 (256 tiles)           6.1    7.3    8.7   12.5
-//   6144 rows x 16 (384 tiles)           8.9    7.6    8.8   12.6
-//   4096 rows x 64 (1024 tiles)                10.6    9.3   12.5
-//   6144 rows x 64 (1536 tiles)                15.4   16.3   12.6
-//   32000 rows x 16                                   18.1   16.7
+//   4096 rows x 16 (256 tiles)           6.1    6.9    8.3   11.9
+//   6144 rows x 16 (384 tiles)           8.6    7.0    8.3   12.0
+//   4096 rows x 64 (1024 tiles)         14.7    9.7    8.6   11.9
+//   6144 rows x 64 (1536 tiles)         19.9   12.6   15.0   12.1
+//   32000 rows x 16                     30.4   19.8   17.8   16.9
 //   tokens of a workgroup of 128 rows      16     32     64
-//   6144 rows x 64 (192, 96, 48 of them) 12.6   16.1   27.3
-//   16384 rows x 64 (512, 256, 128)             17.8   29.1
-//   32000 rows x 64 (1000, 500, 250)     55.8   35.7   29.5
-// What bounds the last (2.5 TB/s, 0.57 PFLOP/s) is issue: the vector ALU is busy
-// for 48 % of the cycles, the matrix pipe for 24 %, two waves a SIMD.  Binary32
-// activations take three times the LDS and products.
+//   6144 rows x 64 (192, 96, 48 of them) 12.2   15.9   24.2
+//   16384 rows x 64 (512, 256, 128)      24.2   18.8   25.4
+//   32000 rows x 64 (1000, 500, 250)     51.3   33.9   26.5
+// What bounds the last (2.8 TB/s, 0.63 PFLOP/s) is issue: some 8 of the 26 us are the
+// launch, the first loads and the results, and of the rest decoding, scales, sums of x
+// and products each cost what leaving them out saves, 1 to 4 us, with two waves a SIMD
+// to overlap them.  Binary32 activations take three times the LDS and products.
 constexpr int kCus = 256;
 
 template <int NU, int GB>
 hipError_t run_linear_16(const LinArgs& a, int64_t tiles, hipStream_t s) {
   if (tiles <= kCus) {
     // long rows at one to four tokens: 16 waves keep more loads under way (14336
-    // columns 9.0 us, with 8 waves 10.7; 4096 columns 4.5 and 4.4)
+    // columns 8.6 us, with 8 waves 10.1; 4096 columns 4.5 and 4.2)
     if constexpr (NU == 1)
       if (a.KB > 48) return run_linear_g<uint16_t, 1, NU, 1, 1, 16, GB>(a, s);
     return run_linear_g<uint16_t, 1, NU, 1, 1, 8, GB>(a, s);
