@@ -432,16 +432,35 @@ hipError_t run_linear_32(const LinArgs& a, int64_t tiles, hipStream_t s) {
   if constexpr (GB < 4) return run_linear_g<float, 1, NU, 1, 4, 4, GB>(a, s);
 }
 
+// Workgroups of 128 rows, or of 256, which take 1.63 times as long and are taken
+// where that saves rounds of workgroups (one a CU): 6144 x 4096 at 256 tokens (192 or
+// 96 workgroups) 24.9 us and 39.4, 32000 x 4096 at 128 (500 or 250) 50.9 and 43.7; fp32,
+// 96 tokens (750 or 375) 91 and 97, 128 (1000 or 500) 122 and 102.
+template <typename TX, int NT, int GB>
+hipError_t run_linear_wide(const LinArgs& a, hipStream_t s) {
+  const int64_t blocks = (a.T - 1) / (16 * NT) + 1;
+  const auto rounds = [&](int tiles) {
+    return (((a.RB - 1) / tiles + 1) * blocks + kCus - 1) / kCus;
+  };
+  if (8 * rounds(16) < 5 * rounds(8)) return run_linear_g<TX, NT, 4 * NT, 2, 8, 1, GB>(a, s);
+  return run_linear_g<TX, NT, 4 * NT, 2, 4, 2, GB>(a, s);
+}
+
 template <int GB>
 hipError_t run_linear(const LinArgs& a, bool x_bf, hipStream_t s) {
   const int64_t tiles = (int64_t)a.RB * ((a.T + 15) / 16);
-  if constexpr (GB < 4) {  // as above
-    const int64_t rows = (a.RB + 7) / 8, enough = kCus * 3 / 4;
+  const int64_t rows = (a.RB + 7) / 8, enough = kCus * 3 / 4;  // as above
+  if constexpr (GB < 4) {
     if (x_bf && a.T > 32 && rows * ((a.T + 63) / 64) >= enough)
-      return run_linear_g<uint16_t, 4, 16, 2, 4, 2, GB>(a, s);
-    if (a.T > 16 && rows * ((a.T + 31) / 32) >= enough)
-      return x_bf ? run_linear_g<uint16_t, 2, 8, 1, 8, 2, GB>(a, s)
-                  : run_linear_g<float, 2, 8, GB == 1 ? 2 : 1, 4, 2, GB>(a, s);
+      return run_linear_wide<uint16_t, 4, GB>(a, s);
+    if (!x_bf && a.T > 16 && rows * ((a.T + 31) / 32) >= enough)
+      return run_linear_wide<float, 2, GB>(a, s);
+  }
+  // groups of 32 need more registers: 32 tokens and one row tile a wave (14336 x
+  // 4096 at 64 tokens 43.8 us with 16 tokens, 26.9 so; fp32 83.7 and 53.7)
+  if (a.T > 16 && rows * ((a.T + 31) / 32) >= enough) {
+    if (x_bf) return run_linear_g<uint16_t, 2, 8, 1, 8, 2, GB>(a, s);
+    if constexpr (GB == 4) return run_linear_g<float, 2, 8, 1, 4, 2, GB>(a, s);
   }
   if (a.T <= 4) return x_bf ? run_linear_16<1, GB>(a, tiles, s) : run_linear_32<1, GB>(a, tiles, s);
   if (a.T <= 8) return x_bf ? run_linear_16<2, GB>(a, tiles, s) : run_linear_32<2, GB>(a, tiles, s);

@@ -94,6 +94,15 @@ def test_many_rows(T, rows, cols, group, x_dtype):
     check(T, rows, cols, group, x_dtype, x_dtype, bias=True, seed=T)
 
 
+# workgroups of 256 rows, the last of them partly filled
+@pytest.mark.parametrize("cols,group", [(160, 32), (192, 64), (384, 128), (1152, 128)])
+@pytest.mark.parametrize("x_dtype", [BF, F32])
+def test_widest_workgroups(cols, group, x_dtype):
+    check(66, 20010, cols, group, x_dtype, F32, bias=True, seed=cols)
+    check(66, 20010, cols, group, x_dtype, BF, bias=False, seed=cols + 1)
+
+
+
 @pytest.mark.parametrize("T", [1, 3, 5, 20])
 @pytest.mark.parametrize("x_dtype", [BF, F32])
 def test_long_rows(T, x_dtype):
