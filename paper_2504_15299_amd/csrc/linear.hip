@@ -462,6 +462,13 @@ hipError_t run_linear(const LinArgs& a, bool x_bf, hipStream_t s) {
     if (x_bf) return run_linear_g<uint16_t, 2, 8, 1, 8, 2, GB>(a, s);
     if constexpr (GB == 4) return run_linear_g<float, 2, 8, 1, 4, 2, GB>(a, s);
   }
+  // 64 rows by 32 tokens between the two, where one round of them covers more than
+  // four tiles a CU (6144 x 4096 at 64 tokens: 12.3 us, with 16 tokens 13.2, with
+  // groups of 64 13.6 and 15.9; 4096 x 4096 at 64, four tiles a CU: 11.6 and 9.3)
+  if constexpr (GB < 4)
+    if (x_bf && a.T > 16 && tiles > 4 * kCus &&
+        (int64_t)((a.RB + 3) / 4) * ((a.T + 31) / 32) <= kCus)
+      return run_linear_g<uint16_t, 2, 8, 1, 4, 4, GB>(a, s);
   if (a.T <= 4) return x_bf ? run_linear_16<1, GB>(a, tiles, s) : run_linear_32<1, GB>(a, tiles, s);
   if (a.T <= 8) return x_bf ? run_linear_16<2, GB>(a, tiles, s) : run_linear_32<2, GB>(a, tiles, s);
   return x_bf ? run_linear_16<4, GB>(a, tiles, s) : run_linear_32<4, GB>(a, tiles, s);

@@ -94,6 +94,14 @@ def test_many_rows(T, rows, cols, group, x_dtype):
     check(T, rows, cols, group, x_dtype, x_dtype, bias=True, seed=T)
 
 
+# workgroups of 64 rows by 32 tokens
+@pytest.mark.parametrize("T,rows", [(50, 5003), (17, 16000)])
+@pytest.mark.parametrize("cols,group", [(64, 64), (1984, 64), (128, 128), (1152, 128)])
+def test_workgroups_of_64_rows(T, rows, cols, group):
+    check(T, rows, cols, group, BF, F32, bias=True, seed=cols)
+    check(T, rows, cols, group, BF, BF, bias=False, seed=cols + 1)
+
+
 # workgroups of 256 rows, the last of them partly filled
 @pytest.mark.parametrize("cols,group", [(160, 32), (192, 64), (384, 128), (1152, 128)])
 @pytest.mark.parametrize("x_dtype", [BF, F32])
