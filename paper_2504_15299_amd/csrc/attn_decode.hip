@@ -678,23 +678,33 @@ bool attn_splits(int B, int q_heads, int n_heads, int dim, int size, int keys, i
          units * ((room < 0x7fffffff ? room : 0x7fffffff) / 16 + 1) < 0x7fffffff;
 }
 
+// Waves of a workgroup that takes a unit whole: eight where the chip has room for
+// them, two where units are many and short, so that more of them are under way (up to
+// 64 keys, 8 heads of 128, bf16, 128 sequences: 10.3 us with four, 7.7 with two, 2000
+// sequences of up to 200 198 and 166; but 64 sequences, two units a CU, of up to 500
+// 18.0 and 18.4, and 300 with 4 heads of up to 3000 201.7 and 202.6; fp32, 128
+// sequences, 12 heads of 64: 64 keys 11.6 and 10.6, 220 keys 22.9 and 25.2).
 template <typename T, int DP, bool PAD, int HT>
-void run_attn_h(const AttnArgs& a, bool split, hipStream_t s) {
+void run_attn_h(const AttnArgs& a, bool split, int keys, hipStream_t s) {
   const int units = a.B * a.H * a.tiles;
+  const bool short_units =
+      (int64_t)keys * DP * sizeof(T) <= (sizeof(T) == 2 ? kWholeBytes / 2 : kWholeBytes / 8);
   if (split)
     attn_decode_kernel<T, DP, PAD, HT, 4, true><<<a.groups, 256, 0, s>>>(a);
-  else if (DP <= 128 && units <= kCus)  // more waves a unit, where the chip has room
+  else if (DP <= 128 && units <= kCus)
     attn_decode_kernel<T, DP, PAD, HT, DP <= 128 ? 8 : 4, false><<<units, 512, 0, s>>>(a);
+  else if (units > 2 * kCus && short_units)
+    attn_decode_kernel<T, DP, PAD, HT, 2, false><<<units, 128, 0, s>>>(a);
   else
     attn_decode_kernel<T, DP, PAD, HT, 4, false><<<units, 256, 0, s>>>(a);
 }
 
 template <typename T, int DP, bool PAD>
-hipError_t run_attn(const AttnArgs& a, bool split, hipStream_t s) {
+hipError_t run_attn(const AttnArgs& a, bool split, int keys, hipStream_t s) {
   if (a.G <= 4)
-    run_attn_h<T, DP, PAD, 4>(a, split, s);
+    run_attn_h<T, DP, PAD, 4>(a, split, keys, s);
   else
-    run_attn_h<T, DP, PAD, 16>(a, split, s);
+    run_attn_h<T, DP, PAD, 16>(a, split, keys, s);
   const hipError_t err = hipGetLastError();
   if (err != hipSuccess || !split) return err;
   constexpr int TK = Tile<T, DP, PAD>::TK;
@@ -709,13 +719,13 @@ hipError_t run_attn(const AttnArgs& a, bool split, hipStream_t s) {
 }
 
 template <typename T>
-hipError_t run_attn_t(const AttnArgs& a, bool split, hipStream_t s) {
-  if (a.D == 64) return run_attn<T, 64, false>(a, split, s);
-  if (a.D < 64) return run_attn<T, 64, true>(a, split, s);
-  if (a.D == 128) return run_attn<T, 128, false>(a, split, s);
-  if (a.D < 128) return run_attn<T, 128, true>(a, split, s);
-  if (a.D == 256) return run_attn<T, 256, false>(a, split, s);
-  return run_attn<T, 256, true>(a, split, s);
+hipError_t run_attn_t(const AttnArgs& a, bool split, int keys, hipStream_t s) {
+  if (a.D == 64) return run_attn<T, 64, false>(a, split, keys, s);
+  if (a.D < 64) return run_attn<T, 64, true>(a, split, keys, s);
+  if (a.D == 128) return run_attn<T, 128, false>(a, split, keys, s);
+  if (a.D < 128) return run_attn<T, 128, true>(a, split, keys, s);
+  if (a.D == 256) return run_attn<T, 256, false>(a, split, keys, s);
+  return run_attn<T, 256, true>(a, split, keys, s);
 }
 
 }  // namespace
@@ -749,8 +759,8 @@ hipError_t launch_attn_decode(const void* q, int64_t q_stride, int B, int q_head
   const int rows = a.G < kHeadTile ? a.G : kHeadTile;
   a.part_o = (float*)ws;
   a.part_ml = (float*)ws + (size_t)a.groups * 2 * rows * a.D;
-  return c->dtype == D2MOE_BF16 ? run_attn_t<uint16_t>(a, split, s)
-                                : run_attn_t<float>(a, split, s);
+  return c->dtype == D2MOE_BF16 ? run_attn_t<uint16_t>(a, split, keys, s)
+                                : run_attn_t<float>(a, split, keys, s);
 }
 
 }  // namespace d2moe

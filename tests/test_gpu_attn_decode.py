@@ -106,6 +106,17 @@ def test_shares(B, Hq, H, D, dtype, max_len):
     check(*make(lengths.tolist(), Hq, H, D, 16, dtype, seed=B), max_len=max_len)
 
 
+# more short units than the chip takes at a time; one sequence longer than expected
+@pytest.mark.parametrize("G", [1, 6])
+@pytest.mark.parametrize("D", [40, 64, 80, 128, 256])
+@pytest.mark.parametrize("dtype", [BF, F32])
+def test_many_short_units(G, D, dtype):
+    rng = np.random.default_rng(D + G)
+    lengths = rng.integers(0, 50, 130)
+    lengths[77] = 1100
+    check(*make(lengths.tolist(), 4 * G, 4, D, 16, dtype, seed=D), max_len=30)
+
+
 @pytest.mark.parametrize("dtype", [BF, F32])
 def test_all_empty(dtype):
     for max_len in (10, 5000):
