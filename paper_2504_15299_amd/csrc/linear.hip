@@ -62,7 +62,7 @@ __device__ inline u4 decode(uint32_t w, uint32_t mask) {
 }
 
 // Eight activations as loaded; the operand(s) they become (NP = 1 for bf16, 3
-// pieces for binary32, smallest first) and their sum.  A piece is the value cut
+// pieces for binary32, smallest first) and their sums.  A piece is the value cut
 // to its upper 16 bits, what is left goes to the next (an infinity leaves NaN).
 template <typename TX>
 struct XRaw;
@@ -72,13 +72,13 @@ struct XRaw<uint16_t> {
   u4 v;
   __device__ void load(const uint16_t* x) { v = *(const u4*)x; }
   __device__ void pieces(u4 (&p)[1]) const { p[0] = v; }
-  __device__ float sum() const {
+  __device__ void sum(float (&s)[1]) const {
     const b2 one = {(__bf16)1.0f, (__bf16)1.0f};
-    float s = 0.0f;
+    s[0] = 0.0f;
 #pragma unroll
     for (int d = 0; d < 4; ++d)
-      s = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(b2, (uint32_t)v[d]), one, s, false);
-    return s;
+      s[0] = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(b2, (uint32_t)v[d]), one, s[0],
+                                             false);
   }
 };
 template <>
@@ -106,9 +106,15 @@ struct XRaw<float> {
       for (int d = 0; d < 4; ++d)
         p[k][d] = __builtin_amdgcn_perm(h[k][2 * d + 1], h[k][2 * d], 0x07060302u);
   }
-  __device__ float sum() const {
-    const f4 s = v[0] + v[1];
-    return (s[0] + s[1]) + (s[2] + s[3]);
+  __device__ void sum(float (&s)[2]) const {  // of the first pieces and of what is left
+    s[0] = s[1] = 0.0f;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const float f = v[e >> 2][e & 3];
+      const float first = __uint_as_float(__float_as_uint(f) & 0xffff0000u);
+      s[0] += first;
+      s[1] += f - first;
+    }
   }
 };
 
@@ -175,13 +181,15 @@ __device__ inline void load_w(WFrag<RT, GB>& f, const LinArgs& a, int rb0, int k
 template <typename TX, int NT, int NU, int RT, int R, int S, int GB>
 __global__ __launch_bounds__(64 * R * S) void linear_kernel(LinArgs a) {
   constexpr int NP = XRaw<TX>::NP, kUnits = (NU + R - 1) / R;
-  // the first pieces of binary32 activations are summed apart from the rest:
-  // their products have 13 bits, so that sum is nearly exact, and what the
-  // 16 + z cancels of it is not rounded at the size of the uncancelled sum
+  // The first pieces of binary32 activations are summed apart from the rest, here and
+  // in the sums of x: they have 8 bits, their products 13, so both sums are nearly
+  // exact, and what the 16 + z cancels of them is not rounded at the size of the
+  // uncancelled sums (one group of 128 columns: errors of 3e-8 of the result, with
+  // one sum of x 1e-6; 16 x 4096 x 4096 takes 11.2 us for it, 10.9 with one).
   constexpr int NA = NP == 1 ? 1 : 2;
   struct Stage {
     u4 x[2][S][NP][NT * 4 * 64];
-    float sum[2][S][GB][NT * 16];
+    float sum[2][S][NA][GB][NT * 16];
   };
   union Lds {
     Stage st;
@@ -225,12 +233,19 @@ __global__ __launch_bounds__(64 * R * S) void linear_kernel(LinArgs a) {
       for (int k = 0; k < NP; ++k)
         lds.st.x[buf][sk][k][((t >> 4) * 4 + (col >> 2)) * 64 + (col & 3) * 16 +
                              ((t & 15) ^ col)] = p[k];
-      float s = x[i].sum();
-      s = dpp_add<0xB1>(s);                        // quads: lane ^ 1, lane ^ 2
-      s = dpp_add<0x4E>(s);
-      if constexpr (GB <= 2) s = dpp_add<0x141>(s);  // halves of a row of 16, mirrored
-      if constexpr (GB == 1) s = dpp_add<0x140>(s);  // the row, mirrored
-      if (col % (16 / GB) == 0) lds.st.sum[buf][sk][col / (16 / GB)][t] = s;
+      float s[NA];
+      x[i].sum(s);
+#pragma unroll
+      for (int h = 0; h < NA; ++h) {
+        s[h] = dpp_add<0xB1>(s[h]);  // quads: lane ^ 1, lane ^ 2
+        s[h] = dpp_add<0x4E>(s[h]);
+        if constexpr (GB <= 2) s[h] = dpp_add<0x141>(s[h]);  // halves of a row of 16, mirrored
+        if constexpr (GB == 1) s[h] = dpp_add<0x140>(s[h]);  // the row, mirrored
+      }
+      if (col % (16 / GB) == 0) {
+#pragma unroll
+        for (int h = 0; h < NA; ++h) lds.st.sum[buf][sk][h][col / (16 / GB)][t] = s[h];
+      }
     }
   };
   // a step's activations are shared by R waves, or stay within one
@@ -279,9 +294,11 @@ __global__ __launch_bounds__(64 * R * S) void linear_kernel(LinArgs a) {
         for (int h = 0; h < NA; ++h)
 #pragma unroll
           for (int r = 0; r < RT; ++r) acc[r][n][h] = zero;
-      float xs[NT];
+      float xs[NT][NA];
 #pragma unroll
-      for (int n = 0; n < NT; ++n) xs[n] = lds.st.sum[buf][sk][g][16 * n + col];
+      for (int n = 0; n < NT; ++n)
+#pragma unroll
+        for (int h = 0; h < NA; ++h) xs[n][h] = lds.st.sum[buf][sk][h][g][16 * n + col];
 #pragma unroll
       for (int jj = 0; jj < 4 / GB; ++jj) {
         const int j = g * (4 / GB) + jj;
@@ -308,8 +325,8 @@ __global__ __launch_bounds__(64 * R * S) void linear_kernel(LinArgs a) {
           const float z = (float)((w.z[r][g] >> (8 * i)) & 255u);  // 16 + zero point
 #pragma unroll
           for (int n = 0; n < NT; ++n) {
-            float v = fmaf(-z, xs[n], acc[r][n][0][i]);
-            if constexpr (NA == 2) v += acc[r][n][1][i];
+            float v = fmaf(-z, xs[n][0], acc[r][n][0][i]);
+            if constexpr (NA == 2) v += fmaf(-z, xs[n][1], acc[r][n][1][i]);
             y[r][n][i] = fmaf(s, v, y[r][n][i]);
           }
         }
@@ -435,7 +452,7 @@ hipError_t run_linear_32(const LinArgs& a, int64_t tiles, hipStream_t s) {
 // Workgroups of 128 rows, or of 256, which take 1.63 times as long and are taken
 // where that saves rounds of workgroups (one a CU): 6144 x 4096 at 256 tokens (192 or
 // 96 workgroups) 24.9 us and 39.4, 32000 x 4096 at 128 (500 or 250) 50.9 and 43.7; fp32,
-// 96 tokens (750 or 375) 91 and 97, 128 (1000 or 500) 122 and 102.
+// 96 tokens (750 or 375) 91 and 97, 128 (1000 or 500) 122 and 104.
 template <typename TX, int NT, int GB>
 hipError_t run_linear_wide(const LinArgs& a, hipStream_t s) {
   const int64_t blocks = (a.T - 1) / (16 * NT) + 1;
@@ -457,7 +474,7 @@ hipError_t run_linear(const LinArgs& a, bool x_bf, hipStream_t s) {
       return run_linear_wide<float, 2, GB>(a, s);
   }
   // groups of 32 need more registers: 32 tokens and one row tile a wave (14336 x
-  // 4096 at 64 tokens 43.8 us with 16 tokens, 26.9 so; fp32 83.7 and 53.7)
+  // 4096 at 64 tokens 43.8 us with 16 tokens, 26.9 so; fp32 83.7 and 59.3)
   if (a.T > 16 && rows * ((a.T + 31) / 32) >= enough) {
     if (x_bf) return run_linear_g<uint16_t, 2, 8, 1, 8, 2, GB>(a, s);
     if constexpr (GB == 4) return run_linear_g<float, 2, 8, 1, 4, 2, GB>(a, s);

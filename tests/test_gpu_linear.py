@@ -94,6 +94,30 @@ def test_many_rows(T, rows, cols, group, x_dtype):
     check(T, rows, cols, group, x_dtype, x_dtype, bias=True, seed=T)
 
 
+@pytest.mark.parametrize("T,rows,cols,group", [(1, 141, 128, 128), (3, 100, 192, 64), (9, 65, 96, 32),
+                                               (20, 300, 640, 128), (40, 12300, 128, 64)])
+def test_float_activations_keep_their_precision(T, rows, cols, group):
+    """Activations of one binade: their first eight bits are multiples of 2^-7, the
+    sums of those times 16 + n, and of those times 16 + z, of 2^13 at most, so both
+    are exact, also where they cancel (most codes equal their zero point).  What is
+    left, below 2^-16 here, has in a group two sums of 2 * group terms of 31 2^-16 at
+    most, each addition off by 2 U of the sum so far."""
+    rng = np.random.default_rng(cols)
+    codes, scales, zeros = weights(rows, cols, group)
+    same = rng.random((rows, cols)) < 0.95
+    codes[same] = np.repeat(zeros, group, 1)[same]
+    x = 1 + rng.integers(0, 128, (T, cols)) / 128 + rng.uniform(0, 2.0 ** -16, (T, cols))
+    x = x.astype(np.float32)
+    y = api.linear_forward(torch.from_numpy(x).to(DEV), packed(codes, scales, zeros, group))
+    x = x.astype(np.float64)
+    want, _ = ref.linear(x, codes, scales, zeros, group)
+    s = scales.astype(np.float64)
+    w = np.repeat(s, group, 1) * (codes.astype(np.float64) - np.repeat(zeros, group, 1))
+    err = (2 * ref.U * 2 * group * 2.0 ** -16) * (62 * group * s.sum(1)) + \
+        (cols // group + 20) * ref.U * (np.abs(x) @ np.abs(w).T)
+    assert (np.abs(y.double().cpu().numpy() - want) <= err).all()
+
+
 # workgroups of 64 rows by 32 tokens
 @pytest.mark.parametrize("T,rows", [(50, 5003), (17, 16000)])
 @pytest.mark.parametrize("cols,group", [(64, 64), (1984, 64), (128, 128), (1152, 128)])
