@@ -485,8 +485,8 @@ d2moe_status d2moe_linear_pack_codes(const uint8_t* codes, const uint16_t* scale
  * Products are exact and summed in binary32 within a group, groups in
  * binary32.  A token with an infinity or NaN among its activations gets NaN or
  * infinite results; other tokens' do not depend on it.  0 <= T <= 2^20; made
- * for the T of a decode step: above 64 tokens the weights are read again for
- * every 64.  The sums are of (16 + n) x, which a group's activations must keep
+ * for the T of a decode step: above 64 tokens (binary32 or groups of 32: 32) the
+ * weights are read again.  The sums are of (16 + n) x, which a group's activations must keep
  * within binary32.  y does not overlap x.  No workspace; results do not depend
  * on what else runs.
  */
