@@ -118,3 +118,44 @@ def test_attention_of_one_head_over_many_parts(dtype):
     err = mag * (2 * ds + 2.0 ** -16 + n * 2.0 ** -24) + \
         want.abs() * torch.finfo(dtype).eps / 2 + 1e-30
     assert ((got[0].double().cpu() - want).abs() <= err).all()
+
+
+def test_two_graphs_share_a_workspace():
+    """Split calls captured over one workspace, replayed in turn with eager work
+    between, follow their inputs: lengths, queries and the cache's new tokens."""
+    B, H, D, page = 3, 2, 128, 16
+    caches = [cache_of(B * 200, page, H, D) for _ in range(2)]
+    table = torch.randperm(B * 200, device=DEV).to(I32).view(B, 200)
+    qkv = torch.randn((B, 8 + 2 * H, D), device=DEV).to(BF)
+    pos = torch.tensor([2500, 30, 1100], dtype=I32, device=DEV)
+    lengths = pos + 1
+    need = api.attn_decode_workspace(B, 8, caches[0], 3000)
+    assert need > 0
+    ws = torch.empty(need, dtype=torch.uint8, device=DEV)
+    outs = [torch.empty((B, 8, D), dtype=BF, device=DEV) for _ in caches]
+
+    def step(c, out, work):
+        api.kv_append(None, qkv[:, 8:8 + H], qkv[:, 8 + H:], c, table, pos)
+        api.attn_decode(qkv[:, :8], c, table, lengths, max_len=3000, out=out, workspace=work)
+
+    graphs = []
+    for c, out in zip(caches, outs):
+        step(c, out, ws)
+        torch.cuda.synchronize()
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            step(c, out, ws)
+        graphs.append(g)
+    for i in range(4):
+        qkv.normal_()
+        pos.copy_(torch.tensor([2600 + i, 31 * i, 1], dtype=I32))
+        lengths.copy_(pos + 1)
+        ws.fill_(255)
+        for g, out in zip(graphs, outs):
+            out.fill_(-7)
+            g.replay()
+        for c, out in zip(caches, outs):
+            want = torch.empty_like(out)
+            step(c, want, torch.empty_like(ws))
+            torch.cuda.synchronize()
+            assert torch.equal(out, want)
