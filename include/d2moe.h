@@ -571,7 +571,8 @@ d2moe_status d2moe_kv_append(const void* q, int64_t q_stride, int32_t q_heads, c
  * -infinity.  Cache rows outside the tokens
  * attended are not used, whatever they hold.  Scores, softmax and sums are
  * binary32; with a bf16 cache the probabilities enter the value product as
- * two bf16 terms.
+ * three bf16 pieces, whose sum is the binary32 probability (below 2^-103, to 2^-132).
+ * A key whose probability is 0 in binary32 adds nothing for finite values.
  */
 d2moe_status d2moe_attn_decode_workspace(int32_t B, int32_t q_heads, int32_t n_heads,
                                          int32_t head_dim, int32_t max_len, size_t* bytes);

@@ -97,8 +97,7 @@ def attn(q, k, v, table, lengths, scale, window=0):
 
     A score is off by 2 U per product of its D terms, the exponent's argument
     by a few U of its size, a probability therefore relatively by twice that
-    (it and the sum), by 2^-16 where it is held in two bf16 terms, and by
-    2 U per key of the sums."""
+    (it and the sum), and by 2 U per key of the sums.  (2^-15 is left on top.)"""
     B, Hq, D = q.shape
     n_pages, page, H, _ = k.shape
     out, err = np.zeros_like(q), np.zeros_like(q)
