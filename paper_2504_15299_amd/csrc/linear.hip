@@ -204,9 +204,9 @@ __global__ __launch_bounds__(64 * R * S) void linear_kernel(LinArgs a) {
 
   // NU units of 4 tokens by 128 columns (fewer than 4 NT where there are no more
   // tokens); a lane has 8 columns of one token.  Tokens past the last repeat it
-  // (their results are not written), and so do columns and blocks (their scales
-  // are taken as zero): every load is made, so that a wait can count on those
-  // behind the one it is for.
+  // (their results are not written), and so do columns (their groups are left out)
+  // and blocks (their scales are taken as zero): every load is made, so that a wait can
+  // count on those behind the one it is for.
   uint32_t xrow[kUnits];
 #pragma unroll
   for (int i = 0; i < kUnits; ++i) {
@@ -316,6 +316,9 @@ __global__ __launch_bounds__(64 * R * S) void linear_kernel(LinArgs a) {
             for (int r = 0; r < RT; ++r) acc[r][n][h] = mma(wa[r], xp[j & 1][n][k], acc[r][n][h]);
           }
       }
+      // a group past the last column: its sums repeat other columns and may overflow
+      // where no group does, so that a scale of zero would not take them out
+      if (GB > 1 && (it * S + sk) * kLinCols + g * (kLinCols / GB) >= a.cols) continue;
 #pragma unroll
       for (int r = 0; r < RT; ++r) {
         const uint2 sc = live ? w.s[r][g] : make_uint2(0, 0);

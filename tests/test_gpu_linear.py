@@ -158,6 +158,23 @@ def test_small_and_large_activations():
     ref.close(y, *ref.linear(x.astype(np.float64), codes, scales, zeros, 128), F32)
 
 
+# every division of the work, its last column block one to three quarters filled
+@pytest.mark.parametrize("T,rows", [(1, 20), (5, 5000), (20, 20), (20, 9000), (40, 12300), (17, 16000),
+                                    (66, 20010)])
+@pytest.mark.parametrize("cols,group", [(32, 32), (96, 32), (64, 64), (192, 64)])
+@pytest.mark.parametrize("x_dtype", [BF, F32])
+def test_large_activations_in_a_last_block_not_filled(T, rows, cols, group, x_dtype):
+    """Eight activations of 1e36 under codes of 15: the sums of their group are 2.5e38
+    at most, within binary32, and nothing may repeat them beyond that."""
+    codes, scales, zeros = weights(rows, cols, group)
+    codes[:, -8:] = 15
+    x = np.random.default_rng(0).standard_normal((T, cols))
+    x[:, -8:] = 1e36
+    x = ref.as_type(x, x_dtype)
+    y = api.linear_forward(x.to(DEV), packed(codes, scales, zeros, group))
+    ref.close(y, *ref.linear(ref.f64(x), codes, scales, zeros, group), x_dtype)
+
+
 @pytest.mark.parametrize("x_dtype", [BF, F32])
 @pytest.mark.parametrize("value", [float("nan"), float("inf"), float("-inf")])
 def test_a_token_that_is_not_finite_stays_alone(x_dtype, value):
