@@ -409,6 +409,8 @@ d2moe_status d2moe_attn_decode(const void* q, int64_t q_stride, int32_t B, int32
   if (!q || !out || !lengths || !aligned(q, 16) || !aligned(out, 16) || q_stride % step != 0 ||
       (B > 1 && q_stride < (int64_t)q_heads * cache->head_dim) || (max_pages > 0 && !block_table))
     return D2MOE_EINVAL;
+  // over its queries: the same rows, which no other workgroup reads
+  if (q == out && B > 1 && q_stride != (int64_t)q_heads * cache->head_dim) return D2MOE_EINVAL;
   const size_t need =
       attn_decode_workspace(B, q_heads, cache->n_heads, cache->head_dim, max_len);
   if (need > 0 && (!workspace || ws_bytes < need || !aligned(workspace, 16)))

@@ -114,6 +114,15 @@ def test_attn_decode_refusals():
     refuses("d2moe_attn_decode", ok, [dict(B=0)], api.OK)
 
 
+def test_attn_decode_over_queries_that_are_not_packed():
+    """A result over strided queries would overwrite rows that are still to be read."""
+    bad = dict(q=FAKE, qs=1024, B=2, h=8, c=cache(), bt=FAKE, mp=300, ln=FAKE, ml=4800, w=0, sc=0.125,
+               o=FAKE, ws=None, n=0, s=None)
+    refuses("d2moe_attn_decode", bad, [dict(), dict(B=64), dict(qs=520), dict(ws=FAKE, n=1 << 30)])
+    # one sequence, packed rows, another result: the workspace is what is missing then
+    refuses("d2moe_attn_decode", bad, [dict(B=1), dict(qs=512), dict(o=2 * FAKE)], api.EWORKSPACE)
+
+
 def test_attn_decode_workspace():
     """Grows with the length expected, so that one made for the longest serves
     them all; a call that does not divide its keys needs none."""
