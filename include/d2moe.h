@@ -564,7 +564,7 @@ d2moe_status d2moe_kv_append(const void* q, int64_t q_stride, int32_t q_heads, c
  *        a larger one, 16-byte aligned, or NULL when that says 0; contents need
  *        no initialisation; calls that may run at the same time need one each
  * q_heads is a multiple of n_heads, B <= 65535, B * q_heads <= 2^22, max_pages *
- * page_size <= 2^30; scale is finite.  A sequence of length 0
+ * page_size <= 2^30; |scale| <= 2e38.  A sequence of length 0
  * (or less) gives zeros; a length beyond the table's row counts as the row's
  * end; a token whose page is outside [0, n_pages) counts as masked, and a row
  * with every token masked gives zeros.  So does a row whose scores are all

@@ -3,6 +3,7 @@
 // the per-device address of the fixed scratch array that the allocation-free
 // forward uses (d2moe_moe_forward_noalloc).
 #include <algorithm>
+#include <cmath>
 #include <mutex>
 #include <vector>
 
@@ -401,7 +402,7 @@ d2moe_status d2moe_attn_decode(const void* q, int64_t q_stride, int32_t B, int32
                                size_t ws_bytes, void* stream) {
   if (!cache_ok(cache) ||
       !attn_shape_ok(B, q_heads, cache->n_heads, cache->head_dim, max_len) || max_pages < 0 ||
-      window < 0 || !(scale - scale == 0.0f) ||
+      window < 0 || !std::isfinite(scale * kLog2e) ||
       (int64_t)max_pages * cache->page_size > (1 << 30))
     return D2MOE_EINVAL;
   if (B == 0) return D2MOE_OK;

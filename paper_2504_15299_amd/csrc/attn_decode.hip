@@ -765,7 +765,7 @@ hipError_t launch_attn_decode(const void* q, int64_t q_stride, int B, int q_head
   const bool split = attn_splits(B, q_heads, c->n_heads, a.D, c->dtype == D2MOE_BF16 ? 2 : 4, keys,
                                  (int64_t)max_pages * c->page_size);
   a.groups = split_groups(head_units(B, q_heads, c->n_heads), a.D);
-  a.scale_log2 = scale * 1.44269504088896340736f;
+  a.scale_log2 = scale * kLog2e;
   a.out = out;
   const int rows = a.G < kHeadTile ? a.G : kHeadTile;
   a.part_o = (float*)ws;

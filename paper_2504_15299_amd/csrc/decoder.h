@@ -40,6 +40,8 @@ hipError_t launch_kv_append(const void* q, int64_t q_stride, int q_heads, const 
                             const float* cos, const float* sin, int n_rot, void* q_out,
                             hipStream_t s);
 
+// scores are scaled in units of log2, scale * kLog2e
+constexpr float kLog2e = 1.44269504088896340736f;
 size_t attn_decode_workspace(int B, int q_heads, int n_heads, int dim, int max_len);
 hipError_t launch_attn_decode(const void* q, int64_t q_stride, int B, int q_heads,
                               const d2moe_kv_cache* c, const int32_t* table, int max_pages,

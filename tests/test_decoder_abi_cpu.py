@@ -114,6 +114,15 @@ def test_attn_decode_refusals():
     refuses("d2moe_attn_decode", ok, [dict(B=0)], api.OK)
 
 
+def test_attn_decode_scale_that_overflows():
+    """Scores are scaled in units of log2, where the largest scales have no number: 0
+    times infinity would take the place of a score of 0."""
+    ok = dict(q=FAKE, qs=512, B=3, h=8, c=cache(), bt=FAKE, mp=300, ln=FAKE, ml=4800, w=0, sc=0.125,
+              o=FAKE, ws=None, n=0, s=None)
+    refuses("d2moe_attn_decode", ok, [dict(sc=2.5e38), dict(sc=-2.5e38), dict(sc=3.4e38)])
+    refuses("d2moe_attn_decode", ok, [dict(sc=2e38), dict(sc=-2e38), dict(sc=0.0)], api.EWORKSPACE)
+
+
 def test_attn_decode_over_queries_that_are_not_packed():
     """A result over strided queries would overwrite rows that are still to be read."""
     bad = dict(q=FAKE, qs=1024, B=2, h=8, c=cache(), bt=FAKE, mp=300, ln=FAKE, ml=4800, w=0, sc=0.125,
