@@ -594,7 +594,7 @@ d2moe_status d2moe_attn_decode(const void* q, int64_t q_stride, int32_t B, int32
  *   gate: device (gate_dtype), token t's row gate_stride * t elements from
  *        the start (gate_stride 0: one row for all tokens), or NULL (ones)
  *   h: device [T][d] (h_dtype; bf16 is rounded to nearest even), or NULL
- *        (only x is updated); may be y when of y's type
+ *        (only x is updated); may be y when of y's type, not x
  * 1 <= d <= 16384, T >= 0, eps >= 0, gate_stride 0 or >= d.  Accumulation is
  * fp32.
  */

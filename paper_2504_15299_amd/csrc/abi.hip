@@ -429,6 +429,8 @@ d2moe_status d2moe_block_norm(float* x, float x_scale, const void* y, d2moe_dtyp
   if (T < 0 || d < 1 || d > norm_max_cols() || !(eps >= 0.0f)) return D2MOE_EINVAL;
   if (!dtype_ok(y_dtype) || !dtype_ok(h_dtype) || !dtype_ok(gate_dtype)) return D2MOE_EINVAL;
   if (gate && gate_stride != 0 && gate_stride < d) return D2MOE_EINVAL;
+  // over y: the same rows of the same type; x has a result of its own
+  if (T > 0 && h && ((h == y && h_dtype != y_dtype) || h == x)) return D2MOE_EINVAL;
   if (T > 0 && (!x || !y)) return D2MOE_EINVAL;
   return from_hip(launch_block_norm(x, x_scale, y, y_dtype, y_scale, post_w, gate, gate_dtype,
                                     gate_stride, pre_w, T, d, eps, h, h_dtype,

@@ -161,6 +161,14 @@ def test_block_norm_refusals():
     refuses("d2moe_block_norm", ok, [dict(T=0)], api.OK)
 
 
+def test_block_norm_over_its_inputs():
+    """h over y of another type would overwrite rows that are still to be read, h over
+    x the residual."""
+    bad = dict(x=FAKE, xs=1.0, y=2 * FAKE, yt=1, ys=1.0, pw=None, g=None, gt=0, gs=0, qw=None, T=3, d=64,
+               eps=1e-5, h=2 * FAKE, ht=1, s=None)
+    refuses("d2moe_block_norm", bad, [dict(yt=0), dict(ht=0), dict(h=FAKE), dict(h=FAKE, ht=0)])
+
+
 def test_host_tensors_are_refused():
     x = torch.zeros((2, 8))
     with pytest.raises(ValueError):
