@@ -578,7 +578,7 @@ def kv_append(q, k: torch.Tensor, v: torch.Tensor, cache: KVCache, block_table: 
     """``d2moe_kv_append``: q [N][q_heads][dim] or None, k and v
     [N][heads][dim] (views with packed heads will do), block_table
     [n_seqs][max_pages], positions [N] and token_seq [N] int32, cos and sin
-    [n_rot][dim/2] float32.  Returns q_out [N][q_heads][dim] of the cache's
+    [n_rot][dim/2] float32 (n_rot >= 1).  Returns q_out [N][q_heads][dim] of the cache's
     type (None without q)."""
     dev, dtype, N, D = cache.index, k.dtype, k.shape[0], cache.head_dim
     shape = (N, cache.n_heads, D)
@@ -600,6 +600,8 @@ def kv_append(q, k: torch.Tensor, v: torch.Tensor, cache: KVCache, block_table: 
     n_seqs, pages = block_table.shape
     i32, f32 = torch.int32, torch.float32
     n_rot = 0 if cos is None else cos.shape[0]
+    if cos is not None and n_rot == 0:  # (an empty tensor has no address, which is no rotation)
+        raise ValueError("cos and sin must have a row")
     _run("d2moe_kv_append", dev, stream, pq, qs, heads, pk, pv, ks, _CODES[dtype], N, cache._ref,
          _arg(block_table, (n_seqs, pages), i32, dev, "block_table"), n_seqs, pages,
          _arg(positions, (N,), i32, dev, "positions"),

@@ -100,6 +100,16 @@ def test_kv_append_refusals():
     refuses("d2moe_kv_append", ok, [dict(t=2), dict(t=-1)], api.EUNSUPPORTED)
 
 
+def test_kv_append_with_an_empty_rotation():
+    """Tokens past the rotation's rows are not written; without any rows they must not be
+    written unrotated."""
+    c = api.KVCache.empty(2, 4, 1, 8, dtype=torch.float32, device="cpu")
+    x, one = torch.zeros((1, 1, 8)), torch.zeros(1, dtype=torch.int32)
+    none = torch.empty((0, 4))
+    with pytest.raises(ValueError, match="a row"):
+        api.kv_append(x, x, x, c, one[None], one, cos=none, sin=none)
+
+
 def test_attn_decode_refusals():
     ok = dict(q=FAKE, qs=512, B=3, h=8, c=cache(), bt=FAKE, mp=300, ln=FAKE, ml=4800, w=0, sc=0.125,
               o=FAKE, ws=FAKE, n=1 << 30, s=None)
