@@ -62,6 +62,17 @@ def test_many_rows(d):
         check(T, d, BF, BF, True, True, "token bf16", 0.9, 0.5, seed=T)
 
 
+# rows that are stored past the caches, of every width's workgroups, whole and ragged
+@pytest.mark.parametrize("T,d", [(17000, 256), (20001, 250), (4200, 1000), (2100, 2048), (2117, 2041),
+                                 (1030, 4096), (1031, 4093), (520, 8192), (600, 8190), (257, 16384),
+                                 (300, 16381)])
+@pytest.mark.parametrize("y_dtype,h_dtype", [(BF, BF), (F32, F32)])
+def test_rows_beyond_the_caches(T, d, y_dtype, h_dtype):
+    assert T * d > 1 << 22
+    check(T, d, y_dtype, h_dtype, True, True, "token bf16", 0.9, 0.5, seed=d)
+    check(T, d, y_dtype, h_dtype, d % 2 == 0, False, None, 1.0, 1.0, seed=T)
+
+
 @pytest.mark.parametrize("T", [1, 2, 65, 301])
 @pytest.mark.parametrize("gate", [None, "row bf16", "token bf16", "token f32",
                                   "token strided bf16", "token strided f32"])

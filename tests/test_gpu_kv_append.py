@@ -88,6 +88,20 @@ def test_heads():
     run(N=300, seqs=4, H=2, Hq=4, D=64, page=32, x_dtype=BF, dtype=BF, rotary=True)
 
 
+# rows that are stored past the caches
+@pytest.mark.parametrize("D", [8, 24, 64, 80, 256])
+@pytest.mark.parametrize("x_dtype,dtype", [(BF, BF), (F32, F32), (F32, BF), (BF, F32)])
+@pytest.mark.parametrize("rotary", [True, False])
+def test_many_tokens(D, x_dtype, dtype, rotary):
+    run(N=300, seqs=5, H=2, Hq=6, D=D, page=16, x_dtype=x_dtype, dtype=dtype, rotary=rotary, seed=D)
+
+
+@pytest.mark.parametrize("x_dtype,dtype", [(BF, BF), (F32, F32), (BF, F32)])
+def test_more_tokens_than_a_grid_has(x_dtype, dtype):
+    """65535 workgroups along the tokens, which the first of them walk on from."""
+    run(N=65535 + 73, seqs=64, H=1, Hq=2, D=8, page=257, x_dtype=x_dtype, dtype=dtype, rotary=True)
+
+
 @pytest.mark.parametrize("dtype", [BF, F32])
 def test_in_place(dtype):
     run(N=9, seqs=3, H=2, Hq=4, D=64, page=5, x_dtype=dtype, dtype=dtype, rotary=True,

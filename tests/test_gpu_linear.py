@@ -57,6 +57,16 @@ def test_quantization(rows, cols, group):
         assert np.array_equal(got, exp)
 
 
+def test_a_weight_that_is_not_a_number():
+    W = np.random.default_rng(0).standard_normal((20, 192), dtype=np.float32)
+    W[3, 7], W[4, 64:] = np.nan, np.nan
+    w = api.linear_pack(torch.from_numpy(W).to(DEV), api.Linear.empty(20, 192, 64, DEV))
+    codes, scales, zeros = ref.linear_quantize(np.where(np.isnan(W), 0, W), 64)
+    codes[np.isnan(W)] = 0
+    for got, exp in zip(buffers(w), ref.linear_layout(codes, scales, zeros, 64)):
+        assert np.array_equal(got, exp)
+
+
 def check(T, rows, cols, group, x_dtype, y_dtype, bias, seed=0, shift=0.0):
     rng = np.random.default_rng(seed)
     codes, scales, zeros = weights(rows, cols, group, seed)
@@ -133,6 +143,51 @@ def test_widest_workgroups(cols, group, x_dtype):
     check(66, 20010, cols, group, x_dtype, F32, bias=True, seed=cols)
     check(66, 20010, cols, group, x_dtype, BF, bias=False, seed=cols + 1)
 
+
+
+# every division of the work, by tokens and rows
+@pytest.mark.parametrize("rows", [5, 40, 4100, 6150, 9001, 17000])
+@pytest.mark.parametrize("tokens", [1, 4, 7, 16, 64, None])
+@pytest.mark.parametrize("cols,group", [(160, 32), (192, 64), (320, 64), (384, 128)])
+@pytest.mark.parametrize("x_dtype", [BF, F32])
+def test_every_weight_and_every_bit(rows, tokens, cols, group, x_dtype):
+    """Token t is 0 but at column t, where it has all the bits of its type: a result is
+    one weight times that.  Its pieces' products with 16 + n, and the sum of the smaller
+    two, have at most 21 bits, all exact, and what the zero point takes off leaves each
+    part exact; their sum and its product with the scale are rounded, U each, and all
+    other terms are 0.  (The pieces of a binary32 activation: without the third 2^-17,
+    2^7 U, would be missing.)  `tokens` at a time, None: all of them."""
+    codes, scales, zeros = weights(rows, cols, group, seed=rows)
+    w = packed(codes, scales, zeros, group)
+    v = ref.as_type(np.random.default_rng(cols).uniform(1, 2, cols) * (-1.0) ** np.arange(cols), x_dtype)
+    x = torch.diag(v).to(DEV)
+    step = tokens or cols
+    y = torch.cat([api.linear_forward(x[t:t + step], w, y_dtype=F32) for t in range(0, cols, step)])
+    s = torch.from_numpy(scales).double().repeat_interleave(group, 1)
+    z = torch.from_numpy(zeros).double().repeat_interleave(group, 1)
+    want = ((s * (torch.from_numpy(codes).double() - z)).t() * v.double()[:, None]).to(DEV)
+    assert ((y.double() - want).abs() <= 2.5 * ref.U * want.abs()).all()
+
+
+@pytest.mark.parametrize("T,rows,cols,group", [(1, 40, 4096, 128), (16, 6144, 4096, 128), (17, 700, 4096, 64),
+                                               (64, 6150, 4032, 64), (64, 16384, 2048, 128),
+                                               (33, 6150, 4064, 32), (128, 4096, 14336, 128),
+                                               (300, 4096, 4096, 64)])
+@pytest.mark.parametrize("x_dtype", [BF, F32])
+def test_whole_numbers_are_exact(T, rows, cols, group, x_dtype):
+    """Activations and scales that are small whole numbers and powers of two: every
+    product and sum, of 31 * 4 * 128 within a group and 15 * 4 * 2 * 14336 at the
+    end, in units of 1 / 2, has less than 24 bits."""
+    rng = np.random.default_rng(cols)
+    codes, _, zeros = weights(rows, cols, group)
+    scales = (2.0 ** rng.integers(-1, 2, (rows, cols // group))).astype(np.float16)
+    x = torch.from_numpy(rng.integers(-4, 5, (T, cols))).to(x_dtype).to(DEV)
+    b = torch.from_numpy(rng.integers(-9, 10, rows)).float().to(DEV)
+    y = api.linear_forward(x, packed(codes, scales, zeros, group), b, y_dtype=F32)
+    s = torch.from_numpy(scales).double().repeat_interleave(group, 1)
+    z = torch.from_numpy(zeros).double().repeat_interleave(group, 1)
+    W = (s * (torch.from_numpy(codes).double() - z)).to(DEV)
+    assert torch.equal(y.double(), x.double() @ W.t().contiguous() + b.double())
 
 
 @pytest.mark.parametrize("T", [1, 3, 5, 20])
