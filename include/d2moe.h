@@ -485,10 +485,10 @@ d2moe_status d2moe_linear_pack_codes(const uint8_t* codes, const uint16_t* scale
  * Products are exact and summed in binary32 within a group, groups in
  * binary32.  A token with an infinity or NaN among its activations gets NaN or
  * infinite results; other tokens' do not depend on it.  0 <= T <= 2^20; made
- * for the T of a decode step: above 64 tokens (binary32 or groups of 32: 32) the
- * weights are read again.  The sums are of (16 + n) x, which a group's activations must keep
- * within binary32.  y does not overlap x.  No workspace; results do not depend
- * on what else runs.
+ * for the T of a decode step: the weights are read once per 16, 32 or 64 tokens, as
+ * many as a workgroup takes (more where the rows alone fill the chip).  The sums
+ * are of (16 + n) x, which a group's activations must keep within binary32.  y does
+ * not overlap x.  No workspace; results do not depend on what else runs.
  */
 d2moe_status d2moe_linear_forward(const void* x, d2moe_dtype x_dtype, int32_t T,
                                   const d2moe_linear* w, const float* bias, void* y,

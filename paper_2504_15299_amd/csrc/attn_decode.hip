@@ -18,7 +18,8 @@
 // O in the workspace, and a second kernel joins the parts.
 //
 // Bound by reading the cache: 4 len head_dim bytes (bf16) per key head against
-// 16-column products that would take a twentieth of that time.
+// 16-column products that keep the matrix units busy for a twelfth of the time (64
+// sequences of 8192 keys).
 #include "decoder.h"
 
 namespace d2moe {
@@ -30,10 +31,19 @@ typedef uint32_t u4 __attribute__((ext_vector_type(4)));
 
 constexpr int kHeadTile = 16;    // query heads of a workgroup
 constexpr int kChunk = 512;      // keys whose row offsets are worked out at a time
+// Units from which none is split: they are many a CU then, and one whole a workgroup
+// is faster, with lengths near max_len (256 sequences of up to 4500 keys, 128 a head,
+// 16 key heads: 831 us whole, 847 split, 32: 1600 and 1634, but 8: 441 and 429) and the
+// more so below it (up to 1000 where 5000 are expected, 8 key heads: 107 and 139, up to
+// 100: 20.6 and 49.5).  The price: one long sequence among short ones goes at the rate
+// of one CU a key head (one of 32000, 255 of 300, 8 key heads: 435 and 106 us).
 constexpr int kMaxSplitUnits = 2048;
 constexpr int kSplitSeqs = 256;  // most sequences of a call whose keys are split
 constexpr int kWholeBytes = 256 << 10;  // of keys: up to here a workgroup takes a unit whole
-constexpr int kMinShare = 4;     // tiles
+// Least tiles of a share, one a wave: with fewer more parts are joined, with more
+// fewer CUs read (3000 keys of one head of 128: 11.1 us with 1, 9.6 with 4, 10.5 with 8;
+// 4096 keys of 8 heads: 12.0 with 1 to 4, 12.2 with 8, 14.0 with 16).
+constexpr int kMinShare = 4;
 constexpr int kCus = 256;
 
 struct AttnArgs {
@@ -657,28 +667,29 @@ int head_tiles(int q_heads, int n_heads) {
 }
 
 int head_units(int B, int q_heads, int n_heads) {
-  return B * n_heads * head_tiles(q_heads, n_heads);  // at most 65535 * 65535 / 2, checked first
+  return B * n_heads * head_tiles(q_heads, n_heads);  // at most B * q_heads, 2^22, checked first
 }
 
 // Workgroups of a call whose keys are split: one per CU, whose four waves keep
-// enough loads under way (1 sequence of 32768 keys, 8 heads of 128: 34.5 us, with
-// two 36.5; 64 ragged ones of up to 8192: 251 us = 5.5 TB/s, with two 260); two
+// enough loads under way (1 sequence of 32768 keys, 8 heads of 128: 32.7 us, with
+// two 33.7; 64 ragged ones of up to 8192: 252 us = 5.5 TB/s, with two 261); two
 // where the units are many and short, so that one's start and end lie under the
-// other's loads (32 sequences of up to 2000 keys, 40 heads: 135 and 128 us), or the
-// rows short.  Eight waves a workgroup are as fast (249 us) or slower (4096 keys of
-// one sequence: 13.2 us, 12.7 with four).
+// other's loads (32 sequences of up to 2000 keys, 40 heads: 133 and 125 us), or the
+// rows short (64 of up to 2000, 8 heads of 64: 46.5 and 36.8).  Eight waves a workgroup
+// were no faster (with two pieces of the probabilities: 249 us against 251, 4096 keys of
+// one sequence 13.2 against 12.7).
 int split_groups(int units, int dim) {
   return kCus * (dim <= 64 || (dim <= 128 && units > 512) ? 2 : 1);
 }
 
 // Whether the keys are split.  Not where a second kernel, the look over all lengths
 // and a cold start of every share cost more than the split saves: up to 256 KB of keys
-// a unit (16 sequences of up to 1000 keys, 8 heads of 128, bf16: whole 13.6 us, split
-// 18.9, up to 2000: 18.8 and 21; 16 of 2000, 64 a head: 16.0 and 20.7, up to 3000: 20.8
-// and 20.2; fp32, 16 of up to 1000, 64 a head: both 16.7, up to 1500: 23.3 and 18.8),
+// a unit (16 sequences of up to 1000 keys, 8 heads of 128, bf16: whole 14.0 us, split
+// 19.1, up to 2000: 23.1 and 21.2; 64 a head, up to 2000: 15.6 and 15.8, up to 3000: 21.8
+// and 20.4; fp32, 16 of up to 1000, 64 a head: 16.9 and 17.3, up to 1500: 23.4 and 19.5),
 // twice that in bf16 where the units fill the chip by themselves (64 of up to 1500,
-// 8 heads of 128: 47.2 and 56.1, but 32 of up to 4096: 70.5 and 64.1; fp32, whose units
-// take longer: 64 of up to 2000, 12 heads of 64: 94.5 and 79.3).  Nor where a row of
+// 8 heads of 128: 47.2 and 57.8, but 32 of up to 4096: 71.4 and 63.2; fp32, whose units
+// take longer: 64 of up to 2000, 12 heads of 64: 94.0 and 80.5).  Nor where a row of
 // tiles could pass 2^31.
 bool attn_splits(int B, int q_heads, int n_heads, int dim, int size, int keys, int64_t room) {
   if (B > kSplitSeqs) return false;
@@ -691,10 +702,10 @@ bool attn_splits(int B, int q_heads, int n_heads, int dim, int size, int keys, i
 
 // Waves of a workgroup that takes a unit whole: eight where the chip has room for
 // them, two where units are many and short, so that more of them are under way (up to
-// 64 keys, 8 heads of 128, bf16, 128 sequences: 10.3 us with four, 7.7 with two, 2000
-// sequences of up to 200 198 and 166; but 64 sequences, two units a CU, of up to 500
-// 18.0 and 18.4, and 300 with 4 heads of up to 3000 201.7 and 202.6; fp32, 128
-// sequences, 12 heads of 64: 64 keys 11.6 and 10.6, 220 keys 22.9 and 25.2).
+// 64 keys, 8 heads of 128, bf16, 128 sequences: 10.7 us with four, 7.9 with two, 2000
+// sequences of up to 200 225 and 189; but 64 sequences, two units a CU, of up to 500
+// 17.8 and 19.3, and 300 with 4 heads of up to 3000 208 both; fp32, 128 sequences, 12
+// heads of 64: 64 keys 11.5 and 10.7, 220 keys 22.8 and 25.0).
 template <typename T, int DP, bool PAD, int HT>
 void run_attn_h(const AttnArgs& a, bool split, int keys, hipStream_t s) {
   const int units = a.B * a.H * a.tiles;
@@ -719,9 +730,9 @@ hipError_t run_attn(const AttnArgs& a, bool split, int keys, hipStream_t s) {
   const hipError_t err = hipGetLastError();
   if (err != hipSuccess || !split) return err;
   constexpr int TK = Tile<T, DP, PAD>::TK;
-  // 16 waves for many parts a unit (100000 keys of one key head: 22.4 us for both
-  // kernels, with four waves 36.9; 32 parts: 11.8 and 12.8), four for few (16 sequences
-  // of up to 4096 keys, 8 heads of 128: 39.7 us, with sixteen 41.0)
+  // 16 waves for many parts a unit (100000 keys of one key head: 21.7 us for both
+  // kernels, with four waves 33.0; 32 parts: 12.0 and 13.0), four for few (16 sequences
+  // of up to 4096 keys, 8 heads of 128: 40.0 us, with sixteen 41.4)
   if (a.groups >= 16 * a.B * a.H * a.tiles)
     attn_join_kernel<T, TK, 16><<<dim3(a.Hq, a.B), 1024, 0, s>>>(a);
   else
@@ -729,6 +740,9 @@ hipError_t run_attn(const AttnArgs& a, bool split, int keys, hipStream_t s) {
   return hipGetLastError();
 }
 
+// Dimensions between two widths load the row's start again for what is missing, from the
+// L1 (64 sequences of up to 4000 keys, 8 heads of 64: 74 us, 80: 104, 96: 106, 112: 130,
+// 128: 123; by their bytes, 80 would take 77 and 96 92 of the 123).
 template <typename T>
 hipError_t run_attn_t(const AttnArgs& a, bool split, int keys, hipStream_t s) {
   if (a.D == 64) return run_attn<T, 64, false>(a, split, keys, s);

@@ -366,8 +366,8 @@ __global__ __launch_bounds__(64 * R * S) void linear_kernel(LinArgs a) {
   lds_barrier();
   constexpr int kQuads = 4 * R * RT;
   if constexpr (NT * RT >= S) {
-    // a quad a thread, where that leaves no thread idle (32000 x 4096 at 64 tokens: 32.8
-    // us with a value a thread, 31.8 so; one token of 4096 x 4096: 4.24 and 4.48)
+    // a quad a thread, where that leaves no thread idle (32000 x 4096 at 64 tokens: 31.1
+    // us with a value a thread, 29.9 so; one token of 4096 x 4096: 4.2 and 4.5)
     for (int o = threadIdx.x; o < kQuads * 16 * NT; o += 64 * R * S) {
       const int i = o % kQuads, t = o / kQuads, row = (blockIdx.x * kQuads + i) * 4;
       if (row >= a.rows || t0 + t >= a.T) continue;
@@ -415,26 +415,28 @@ hipError_t run_linear_g(const LinArgs& a, hipStream_t s) {
 // the activations (whose reading from L2 bounds the kernel otherwise) while one
 // round of workgroups fills the chip.  Measured, bf16, 4096 columns, group 128, us:
 //   R, S of 16-token workgroups         1, 8   2, 4   4, 4   8, 2
-//   4096 rows x 16 (256 tiles)           6.1    6.9    8.3   11.9
-//   6144 rows x 16 (384 tiles)           8.6    7.0    8.3   12.0
-//   4096 rows x 64 (1024 tiles)         14.7    9.7    8.6   11.9
-//   6144 rows x 64 (1536 tiles)         19.9   12.6   15.0   12.1
-//   32000 rows x 16                     30.4   19.8   17.8   16.9
+//   4096 rows x 16 (256 tiles)           6.0    6.8    8.3   12.0
+//   6144 rows x 16 (384 tiles)           8.7    7.0    8.4   12.0
+//   4096 rows x 64 (1024 tiles)         14.3    9.8    8.5   12.0
+//   6144 rows x 64 (1536 tiles)         19.8   12.6   15.1   12.1
+//   32000 rows x 16                     29.1   19.2   17.5   16.8
 //   tokens of a workgroup of 128 rows      16     32     64
-//   6144 rows x 64 (192, 96, 48 of them) 12.2   15.9   24.2
-//   16384 rows x 64 (512, 256, 128)      24.2   18.8   25.4
-//   32000 rows x 64 (1000, 500, 250)     51.3   33.9   26.5
-// What bounds the last (2.8 TB/s, 0.63 PFLOP/s) is issue: some 8 of the 26 us are the
-// launch, the first loads and the results, and of the rest decoding, scales, sums of x
-// and products each cost what leaving them out saves, 1 to 4 us, with two waves a SIMD
-// to overlap them.  Binary32 activations take three times the LDS and products.
+//   6144 rows x 64 (192, 96, 48 of them) 12.1   15.9   24.2
+//   16384 rows x 64 (512, 256, 128)      24.2   18.1   25.5
+//   32000 rows x 64 (1000, 500, 250)     50.7   34.4   26.7
+// What bounds the last (2.6 TB/s, 0.63 PFLOP/s) is issue more than any unit: vector
+// instructions take 53 % of the issue slots, the matrix units are busy for 28 % of the
+// cycles, and of the waves, two a SIMD, 28 % wait and 32 % could not issue.  Some 8 of
+// the 27 us are the launch, the first loads and the results, and of the rest decoding,
+// scales, sums of x and products each cost what leaving them out saves, 1 to 4 us.
+// Binary32 activations take three times the LDS and products.
 constexpr int kCus = 256;
 
 template <int NU, int GB>
 hipError_t run_linear_16(const LinArgs& a, int64_t tiles, hipStream_t s) {
   if (tiles <= kCus) {
     // long rows at one to four tokens: 16 waves keep more loads under way (14336
-    // columns 8.6 us, with 8 waves 10.1; 4096 columns 4.5 and 4.2)
+    // columns 9.1 us, with 8 waves 10.3; 4096 columns 4.5 and 4.2)
     if constexpr (NU == 1)
       if (a.KB > 48) return run_linear_g<uint16_t, 1, NU, 1, 1, 16, GB>(a, s);
     return run_linear_g<uint16_t, 1, NU, 1, 1, 8, GB>(a, s);
@@ -454,8 +456,8 @@ hipError_t run_linear_32(const LinArgs& a, int64_t tiles, hipStream_t s) {
 
 // Workgroups of 128 rows, or of 256, which take 1.63 times as long and are taken
 // where that saves rounds of workgroups (one a CU): 6144 x 4096 at 256 tokens (192 or
-// 96 workgroups) 24.9 us and 39.4, 32000 x 4096 at 128 (500 or 250) 50.9 and 43.7; fp32,
-// 96 tokens (750 or 375) 91 and 97, 128 (1000 or 500) 122 and 104.
+// 96 workgroups) 24.8 us and 39.4, 32000 x 4096 at 128 (500 or 250) 51.0 and 44.9; fp32,
+// 96 tokens (750 or 375) 93 and 101, 128 (1000 or 500) 124 and 106.
 template <typename TX, int NT, int GB>
 hipError_t run_linear_wide(const LinArgs& a, hipStream_t s) {
   const int64_t blocks = (a.T - 1) / (16 * NT) + 1;
@@ -477,14 +479,15 @@ hipError_t run_linear(const LinArgs& a, bool x_bf, hipStream_t s) {
       return run_linear_wide<float, 2, GB>(a, s);
   }
   // groups of 32 need more registers: 32 tokens and one row tile a wave (14336 x
-  // 4096 at 64 tokens 43.8 us with 16 tokens, 26.9 so; fp32 83.7 and 59.3)
+  // 4096 at 64 tokens 43.9 us with 16 tokens, 27.3 so; fp32 91.1 and 61.0)
   if (a.T > 16 && rows * ((a.T + 31) / 32) >= enough) {
     if (x_bf) return run_linear_g<uint16_t, 2, 8, 1, 8, 2, GB>(a, s);
     if constexpr (GB == 4) return run_linear_g<float, 2, 8, 1, 4, 2, GB>(a, s);
   }
   // 64 rows by 32 tokens between the two, where one round of them covers more than
-  // four tiles a CU (6144 x 4096 at 64 tokens: 12.3 us, with 16 tokens 13.2, with
-  // groups of 64 13.6 and 15.9; 4096 x 4096 at 64, four tiles a CU: 11.6 and 9.3)
+  // four tiles a CU (at 64 tokens, 4096 columns, 6144 rows: 11.5 us, with 16 tokens 12.3,
+  // 8192 rows 11.8 and 12.5, groups of 64: 13.1 and 15.3, 13.4 and 15.5; 4096 rows, four
+  // tiles a CU: 11.2 and 8.7)
   if constexpr (GB < 4)
     if (x_bf && a.T > 16 && tiles > 4 * kCus &&
         (int64_t)((a.RB + 3) / 4) * ((a.T + 31) / 32) <= kCus)
