@@ -250,7 +250,8 @@ struct Tile<uint16_t, DP, PAD> : KeyRows<uint16_t, DP, 32> {
   // 2^-126 and more; below 2^-103 the last pieces are denormals, which the products
   // take as they are, and no less than the least of those, 2^-133.  16 sequences of up
   // to 4096 keys, 8 heads of 128: 39.8 us with two pieces, 40.3 with three; 64 of up to
-  // 2000, 4 heads of 256: 68.7 and 73.0; 16 of up to 2000, 8 of 64: 14.7 and 15.8; 64 of 8192, 8 heads of 128: 377.5 both.
+  // 2000, 4 heads of 256: 68.7 and 73.0; 16 of up to 2000, 8 of 64: 14.7 and 15.8; 64 of
+  // 8192, 8 heads of 128: 377.5 both.
   __device__ static uint32_t upper(uint32_t second, uint32_t first) {
     return __builtin_amdgcn_perm(second, first, 0x07060302u);
   }
