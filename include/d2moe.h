@@ -548,6 +548,30 @@ d2moe_status d2moe_kv_append(const void* q, int64_t q_stride, int32_t q_heads, c
                              int32_t n_rot, void* q_out, void* stream);
 
 /*
+ * d2moe_kv_append with the norms of the query and key heads before the rotation,
+ * and rotations of part of a head or of neighbouring values:
+ *     x <- weight * x / sqrt(mean_i x_i^2 + eps)     over each head of q and of k,
+ * then the pairs among its first rot_dim values rotated as there, value i with
+ * i + rot_dim/2, or 2 i with 2 i + 1 when interleaved is 1; the values from rot_dim on
+ * stay as they are.  The arithmetic is binary32, rounded once to the cache's type.
+ *   q_weight, k_weight: device [head_dim] float, 16-byte aligned, or NULL (no norm of
+ *        the queries, or of the keys); eps >= 0
+ *   cos, sin: device [n_rot][rot_dim/2] float, both or neither (no rotation); any
+ *        angles will do, so scaled positions are a matter of these tables
+ *   rot_dim: 4..head_dim, a multiple of 4; not looked at without cos and sin
+ * Everything else as d2moe_kv_append: of a token outside the table, the rotation or
+ * the cache, only the query row is written, normed.
+ */
+d2moe_status d2moe_kv_append_norm(const void* q, int64_t q_stride, int32_t q_heads, const void* k,
+                                  const void* v, int64_t kv_stride, d2moe_dtype x_dtype, int32_t N,
+                                  const d2moe_kv_cache* cache, const int32_t* block_table,
+                                  int32_t n_seqs, int32_t max_pages, const int32_t* positions,
+                                  const int32_t* token_seq, const float* q_weight,
+                                  const float* k_weight, float eps, const float* cos,
+                                  const float* sin, int32_t n_rot, int32_t rot_dim,
+                                  int32_t interleaved, void* q_out, void* stream);
+
+/*
  * Attention of one new token per sequence over the paged cache:
  *     out[b][h] = sum_j softmax_j(scale q[b][h] . K_j) V_j,
  * j over the sequence's tokens max(0, n - window) .. n - 1, n = lengths[b]

@@ -107,13 +107,15 @@ def lib():
         L.d2moe_linear_forward.argtypes = [_P, _I, _I, lin, _P, _P, _I, _P]
         L.d2moe_kv_append.argtypes = [_P, i64, _I, _P, _P, i64, _I, _I, kvc, _P, _I, _I, _P, _P,
                                       _P, _P, _I, _P, _P]
+        L.d2moe_kv_append_norm.argtypes = [_P, i64, _I, _P, _P, i64, _I, _I, kvc, _P, _I, _I, _P, _P,
+                                           _P, _P, f32, _P, _P, _I, _I, _I, _P, _P]
         L.d2moe_attn_decode_workspace.argtypes = [_I, _I, _I, _I, _I, sz]
         L.d2moe_attn_decode.argtypes = [_P, i64, _I, _I, kvc, _P, _I, _P, _I, _I, f32, _P, _P,
                                         size, _P]
         L.d2moe_block_norm.argtypes = [_P, f32, _P, _I, f32, _P, _P, _I, i64, _P, _I, _I, f32, _P,
                                        _I, _P]
         for name in ("d2moe_linear_size", "d2moe_linear_pack", "d2moe_linear_pack_codes",
-                     "d2moe_linear_forward", "d2moe_kv_append", "d2moe_attn_decode_workspace",
+                     "d2moe_linear_forward", "d2moe_kv_append", "d2moe_kv_append_norm", "d2moe_attn_decode_workspace",
                      "d2moe_attn_decode", "d2moe_block_norm",
                      "d2moe_mwq_size", "d2moe_pack_mwq", "d2moe_debug_unpack", "d2moe_route",
                      "d2moe_mwq_calib_factor_workspace", "d2moe_mwq_calib_factor",
@@ -572,14 +574,9 @@ def _rows(t, shape, dtype, dev, what):
     return t.data_ptr(), row if n > 1 else heads * dim
 
 
-def kv_append(q, k: torch.Tensor, v: torch.Tensor, cache: KVCache, block_table: torch.Tensor,
-              positions: torch.Tensor, token_seq: torch.Tensor | None = None, cos=None, sin=None,
-              q_out: torch.Tensor | None = None, stream=None):
-    """``d2moe_kv_append``: q [N][q_heads][dim] or None, k and v
-    [N][heads][dim] (views with packed heads will do), block_table
-    [n_seqs][max_pages], positions [N] and token_seq [N] int32, cos and sin
-    [n_rot][dim/2] float32 (n_rot >= 1).  Returns q_out [N][q_heads][dim] of the cache's
-    type (None without q)."""
+def _append_args(q, k, v, cache, q_out, stream):
+    """(q, its stride and heads, k, v, their stride, type code, tokens), q_out and its
+    pointer, of a call that appends."""
     dev, dtype, N, D = cache.index, k.dtype, k.shape[0], cache.head_dim
     shape = (N, cache.n_heads, D)
     pk, ks = _rows(k, shape, dtype, dev, "k")
@@ -597,17 +594,62 @@ def kv_append(q, k: torch.Tensor, v: torch.Tensor, cache: KVCache, block_table: 
             po = q_out.data_ptr()
         else:
             po = _arg(q_out, (N, heads, D), cache.k.dtype, dev, "q_out")
+    return (pq, qs, heads, pk, pv, ks, _CODES[dtype], N), q_out, po
+
+
+def _place_args(N, cache, block_table, positions, token_seq):
+    """The table with its sizes, positions and sequences of a call that appends."""
     n_seqs, pages = block_table.shape
-    i32, f32 = torch.int32, torch.float32
+    dev, i32 = cache.index, torch.int32
+    return (_arg(block_table, (n_seqs, pages), i32, dev, "block_table"), n_seqs, pages,
+            _arg(positions, (N,), i32, dev, "positions"),
+            None if token_seq is None else _arg(token_seq, (N,), i32, dev, "token_seq"))
+
+
+def _turn_args(cos, sin, half, dev):
+    """cos, sin and their rows; half the rotated values: columns, when given."""
+    if cos is None and sin is None:
+        return None, None, 0
     n_rot = 0 if cos is None else cos.shape[0]
     if cos is not None and n_rot == 0:  # (an empty tensor has no address, which is no rotation)
         raise ValueError("cos and sin must have a row")
-    _run("d2moe_kv_append", dev, stream, pq, qs, heads, pk, pv, ks, _CODES[dtype], N, cache._ref,
-         _arg(block_table, (n_seqs, pages), i32, dev, "block_table"), n_seqs, pages,
-         _arg(positions, (N,), i32, dev, "positions"),
-         None if token_seq is None else _arg(token_seq, (N,), i32, dev, "token_seq"),
-         None if cos is None else _arg(cos, (n_rot, D // 2), f32, dev, "cos"),
-         None if sin is None else _arg(sin, (n_rot, D // 2), f32, dev, "sin"), n_rot, po)
+    return (None if cos is None else _arg(cos, (n_rot, half), torch.float32, dev, "cos"),
+            None if sin is None else _arg(sin, (n_rot, half), torch.float32, dev, "sin"), n_rot)
+
+
+def kv_append(q, k: torch.Tensor, v: torch.Tensor, cache: KVCache, block_table: torch.Tensor,
+              positions: torch.Tensor, token_seq: torch.Tensor | None = None, cos=None, sin=None,
+              q_out: torch.Tensor | None = None, stream=None):
+    """``d2moe_kv_append``: q [N][q_heads][dim] or None, k and v
+    [N][heads][dim] (views with packed heads will do), block_table
+    [n_seqs][max_pages], positions [N] and token_seq [N] int32, cos and sin
+    [n_rot][dim/2] float32 (n_rot >= 1).  Returns q_out [N][q_heads][dim] of the cache's
+    type (None without q)."""
+    rows, q_out, po = _append_args(q, k, v, cache, q_out, stream)
+    _run("d2moe_kv_append", cache.index, stream, *rows, cache._ref,
+         *_place_args(rows[-1], cache, block_table, positions, token_seq),
+         *_turn_args(cos, sin, cache.head_dim // 2, cache.index), po)
+    return q_out
+
+
+def kv_append_norm(q, k: torch.Tensor, v: torch.Tensor, cache: KVCache, block_table: torch.Tensor,
+                   positions: torch.Tensor, token_seq: torch.Tensor | None = None, q_weight=None,
+                   k_weight=None, eps: float = 1e-6, cos=None, sin=None, interleaved: bool = False,
+                   q_out: torch.Tensor | None = None, stream=None):
+    """``d2moe_kv_append_norm``: kv_append with RMS norms of the heads of q and k
+    before the rotation, q_weight and k_weight [dim] float32 (None: no norm of
+    these).  cos and sin [n_rot][half] float32 rotate the first 2 * half values of a
+    head (half even, at most dim/2), value i with i + half, or neighbours when
+    ``interleaved``."""
+    rows, q_out, po = _append_args(q, k, v, cache, q_out, stream)
+    dev, D = cache.index, cache.head_dim
+    half = 0 if cos is None else cos.shape[1]
+    f32 = torch.float32
+    _run("d2moe_kv_append_norm", dev, stream, *rows, cache._ref,
+         *_place_args(rows[-1], cache, block_table, positions, token_seq),
+         None if q_weight is None else _arg(q_weight, (D,), f32, dev, "q_weight"),
+         None if k_weight is None else _arg(k_weight, (D,), f32, dev, "k_weight"), eps,
+         *_turn_args(cos, sin, half, dev), 2 * half, int(interleaved), po)
     return q_out
 
 

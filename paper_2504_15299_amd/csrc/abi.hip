@@ -354,12 +354,12 @@ d2moe_status d2moe_linear_forward(const void* x, d2moe_dtype x_dtype, int32_t T,
   return from_hip(launch_linear(x, x_dtype, T, w, bias, y, y_dtype, (hipStream_t)stream));
 }
 
-d2moe_status d2moe_kv_append(const void* q, int64_t q_stride, int32_t q_heads, const void* k,
-                             const void* v, int64_t kv_stride, d2moe_dtype x_dtype, int32_t N,
-                             const d2moe_kv_cache* cache, const int32_t* block_table,
-                             int32_t n_seqs, int32_t max_pages, const int32_t* positions,
-                             const int32_t* token_seq, const float* cos, const float* sin,
-                             int32_t n_rot, void* q_out, void* stream) {
+static d2moe_status append_check(const void* q, int64_t q_stride, int32_t q_heads, const void* k,
+                                 const void* v, int64_t kv_stride, d2moe_dtype x_dtype, int32_t N,
+                                 const d2moe_kv_cache* cache, const int32_t* block_table,
+                                 int32_t n_seqs, int32_t max_pages, const int32_t* positions,
+                                 const float* cos, const float* sin, int32_t n_rot,
+                                 const void* q_out) {
   if (!dtype_ok(x_dtype)) return D2MOE_EUNSUPPORTED;
   if (N < 0 || N > (1 << 30) || !cache_ok(cache) || n_seqs < 0 || max_pages < 0)
     return D2MOE_EINVAL;
@@ -377,9 +377,45 @@ d2moe_status d2moe_kv_append(const void* q, int64_t q_stride, int32_t q_heads, c
   // in place: the same rows of the same type
   if (q && q == q_out && (x_dtype != cache->dtype || (N > 1 && q_stride != q_heads * D)))
     return D2MOE_EINVAL;
+  return D2MOE_OK;
+}
+
+d2moe_status d2moe_kv_append(const void* q, int64_t q_stride, int32_t q_heads, const void* k,
+                             const void* v, int64_t kv_stride, d2moe_dtype x_dtype, int32_t N,
+                             const d2moe_kv_cache* cache, const int32_t* block_table,
+                             int32_t n_seqs, int32_t max_pages, const int32_t* positions,
+                             const int32_t* token_seq, const float* cos, const float* sin,
+                             int32_t n_rot, void* q_out, void* stream) {
+  const d2moe_status st =
+      append_check(q, q_stride, q_heads, k, v, kv_stride, x_dtype, N, cache, block_table, n_seqs,
+                   max_pages, positions, cos, sin, n_rot, q_out);
+  if (st != D2MOE_OK || N == 0) return st;
   return from_hip(launch_kv_append(q, q_stride, q_heads, k, v, kv_stride, x_dtype, N, cache,
                                    block_table, n_seqs, max_pages, positions, token_seq, cos, sin,
                                    n_rot, q_out, (hipStream_t)stream));
+}
+
+d2moe_status d2moe_kv_append_norm(const void* q, int64_t q_stride, int32_t q_heads, const void* k,
+                                  const void* v, int64_t kv_stride, d2moe_dtype x_dtype, int32_t N,
+                                  const d2moe_kv_cache* cache, const int32_t* block_table,
+                                  int32_t n_seqs, int32_t max_pages, const int32_t* positions,
+                                  const int32_t* token_seq, const float* q_weight,
+                                  const float* k_weight, float eps, const float* cos,
+                                  const float* sin, int32_t n_rot, int32_t rot_dim,
+                                  int32_t interleaved, void* q_out, void* stream) {
+  const d2moe_status st =
+      append_check(q, q_stride, q_heads, k, v, kv_stride, x_dtype, N, cache, block_table, n_seqs,
+                   max_pages, positions, cos, sin, n_rot, q_out);
+  if (st != D2MOE_OK) return st;
+  if (!(eps >= 0.0f) || (q_weight && !aligned(q_weight, 16)) ||
+      (k_weight && !aligned(k_weight, 16)) || (interleaved != 0 && interleaved != 1) ||
+      (cos && (rot_dim < 4 || rot_dim > cache->head_dim || rot_dim % 4 != 0)))
+    return D2MOE_EINVAL;
+  if (N == 0) return D2MOE_OK;
+  return from_hip(launch_kv_append_norm(q, q_stride, q_heads, k, v, kv_stride, x_dtype, N, cache,
+                                        block_table, n_seqs, max_pages, positions, token_seq,
+                                        q_weight, k_weight, eps, cos, sin, n_rot, rot_dim,
+                                        interleaved != 0, q_out, (hipStream_t)stream));
 }
 
 static bool attn_shape_ok(int B, int q_heads, int n_heads, int dim, int max_len) {

@@ -40,6 +40,14 @@ hipError_t launch_kv_append(const void* q, int64_t q_stride, int q_heads, const 
                             const float* cos, const float* sin, int n_rot, void* q_out,
                             hipStream_t s);
 
+hipError_t launch_kv_append_norm(const void* q, int64_t q_stride, int q_heads, const void* k,
+                                 const void* v, int64_t kv_stride, d2moe_dtype xd, int N,
+                                 const d2moe_kv_cache* c, const int32_t* table, int n_seqs,
+                                 int max_pages, const int32_t* positions, const int32_t* token_seq,
+                                 const float* q_weight, const float* k_weight, float eps,
+                                 const float* cos, const float* sin, int n_rot, int rot_dim,
+                                 bool interleaved, void* q_out, hipStream_t s);
+
 // scores are scaled in units of log2, scale * kLog2e
 constexpr float kLog2e = 1.44269504088896340736f;
 size_t attn_decode_workspace(int B, int q_heads, int n_heads, int dim, int max_len);
