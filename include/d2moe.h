@@ -227,6 +227,34 @@ d2moe_status d2moe_route_learned(const void* x, d2moe_dtype x_dtype, int32_t T,
                                  void* stream);
 
 /*
+ * Dual routing with the scores of fine-grained MoE decoders in place of the softmax
+ * over the chosen logits.  Of token t's logits l (as d2moe_route computes them from
+ * x, Wg and bias; with x NULL, out->logits holds them and they are read only):
+ *     score_e = softmax_e(l)  or  1 / (1 + exp(-l_e))     (scoring)
+ *     by_e    = score_e + select_bias[e]
+ * The experts stand in `groups` groups of E / groups neighbours; a group's value is
+ * the sum of its two largest by_e (of one, where it has one), and only the experts of
+ * the top_groups best groups take part (groups = top_groups = 1: all).  The k largest
+ * by_e are chosen, ties to the lower index, of groups too, and weigh
+ *     topk_w = scale * score_e,  with renorm 1 divided by the sum of the k scores.
+ * Scores, sums and comparisons are binary64.  A logit of -infinity has a score of 0; a
+ * softmax over nothing else gives scores of 0, and scores that sum to 0 give weights of
+ * 0; logits of +infinity share a softmax's whole.  An expert with a NaN is chosen last
+ * (its own score is NaN, the others' do not depend on it).  Bit-widths, counts, scan, permutation and flags are those of
+ * d2moe_route.
+ *   select_bias: device [E] float or NULL (zeros)
+ * 1 <= k <= top_groups * (E / groups), E % groups == 0, E <= 64, scale finite.
+ */
+typedef enum { D2MOE_SOFTMAX = 0, D2MOE_SIGMOID = 1 } d2moe_scoring;
+d2moe_status d2moe_route_scored(const void* x, d2moe_dtype x_dtype, int32_t T, int32_t d,
+                                const float* Wg, const float* bias, int32_t E, int32_t k,
+                                int32_t scoring, const float* select_bias, int32_t groups,
+                                int32_t top_groups, int32_t renorm, float scale,
+                                const int32_t* token_req, const uint8_t* bit_table, int32_t R,
+                                int32_t b_min, int32_t b_max, const d2moe_routing* out,
+                                void* stream);
+
+/*
  * Workspace bytes needed by d2moe_moe_forward for these sizes (host): the
  * (expert, bit-width) work lists built from the counts B_{j,k} of Sec. 3.4.3,
  * the intermediate SwiGLU activations and expert outputs of the routed

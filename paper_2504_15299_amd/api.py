@@ -10,7 +10,7 @@ from __future__ import annotations
 
 import ctypes
 import os
-from dataclasses import dataclass
+from dataclasses import dataclass, replace
 
 import torch
 
@@ -81,6 +81,9 @@ def lib():
                                   ctypes.POINTER(_Routing), _P]
         L.d2moe_route_learned.argtypes = [_P, _I, _I, _I, _P, _P, _I, _I, _P, _P, _I, _I, _P,
                                           ctypes.POINTER(_Routing), _P]
+        L.d2moe_route_scored.argtypes = [_P, _I, _I, _I, _P, _P, _I, _I, _I, _P, _I, _I, _I,
+                                         ctypes.c_float, _P, _P, _I, _I, _I,
+                                         ctypes.POINTER(_Routing), _P]
         L.d2moe_moe_forward_workspace.argtypes = [_I, _I, _I, _I, _I, _I, sz]
         L.d2moe_moe_forward.argtypes = [_P, _I, _I, _I, _I, _I, _I, ctypes.POINTER(_Mwq),
                                         ctypes.POINTER(_Mwq), ctypes.POINTER(_Routing),
@@ -120,7 +123,7 @@ def lib():
                      "d2moe_mwq_size", "d2moe_pack_mwq", "d2moe_debug_unpack", "d2moe_route",
                      "d2moe_mwq_calib_factor_workspace", "d2moe_mwq_calib_factor",
                      "d2moe_pack_mwq_calibrated_workspace", "d2moe_pack_mwq_calibrated",
-                     "d2moe_route_learned",
+                     "d2moe_route_learned", "d2moe_route_scored",
                      "d2moe_moe_forward_workspace", "d2moe_moe_forward",
                      "d2moe_moe_forward_profiled", "d2moe_moe_forward_noalloc",
                      "d2moe_residual_rmsnorm", "d2moe_stream_read", "d2moe_hebf_order",
@@ -332,6 +335,65 @@ def route_learned(x: torch.Tensor, Wg: torch.Tensor, bias, k: int, Wr: torch.Ten
                                      _ptr(Wr), _ptr(br), b_min, b_max, _ptr(bit_logits),
                                      ctypes.byref(c), _stream(stream)))
     return out, bit_logits
+
+
+_SCORING = {"softmax": 0, "sigmoid": 1}
+_ROUTING_FIELDS = [f for f, _ in _Routing._fields_]
+
+
+def route_scored(logits, k: int, token_req, bit_table: torch.Tensor, scoring: str = "softmax",
+                 select_bias: torch.Tensor | None = None, groups: int = 1, top_groups: int = 1,
+                 renorm: bool = True, scale: float = 1.0, x: torch.Tensor | None = None,
+                 Wg: torch.Tensor | None = None, bias=None, b_min=2, b_max=8,
+                 out: Routing | None = None, stream=None) -> Routing:
+    """``d2moe_route_scored``: experts by scores of ``logits`` [T][E] float32, or, with
+    ``logits`` None, of x [T][d] Wg [E][d]^T + bias.  ``scoring`` is "softmax" or
+    "sigmoid", select_bias [E] float32 or None, token_req [T] int32 or None, bit_table
+    [R][E] uint8.  The routing's ``logits`` are the ones given (those of ``out`` are left
+    alone), or the ones computed."""
+    if scoring not in _SCORING:
+        raise ValueError(f'scoring must be "softmax" or "sigmoid", got {scoring!r}')
+    f32, dev = torch.float32, bit_table.get_device()
+    px, pw, pb, code, d = None, None, None, D2MOE_F32, 0
+    if logits is not None:
+        if x is not None or Wg is not None or bias is not None:
+            raise ValueError("logits, or x and Wg with their bias, not both")
+        T, E = logits.shape
+        pl = _arg(logits, (T, E), f32, dev, "logits")
+    else:
+        if x is None or Wg is None:
+            raise ValueError("logits, or x and Wg, must be given")
+        (T, d), E = x.shape, Wg.shape[0]
+        if x.dtype not in _CODES:
+            raise TypeError(f"unsupported dtype {x.dtype}")
+        px, code = _arg(x, (T, d), x.dtype, dev, "x"), _CODES[x.dtype]
+        pw = _arg(Wg, (E, d), f32, dev, "Wg")
+        pb = None if bias is None else _arg(bias, (E,), f32, dev, "bias")
+    R, L = bit_table.shape[0], b_max - b_min + 1
+    i32, u8 = torch.int32, torch.uint8
+    shapes = [((T, E), f32), ((T, k), i32), ((T, k), f32), ((T, k), u8), ((E, L), i32),
+              ((E * L + 1,), i32), ((T * k,), i32), ((T * k,), i32), ((E,), u8), ((1,), i32)]
+    given = range(len(shapes)) if logits is None else range(1, len(shapes))
+    if out is None:
+        if b_min > b_max or k < 1:
+            raise ValueError("b_min <= b_max and k >= 1 are needed")
+        made = [logits] + [None] * 9
+        for i in given:
+            made[i] = _new(bit_table, *shapes[i], stream)
+        out = Routing(*made)
+    ptrs = [None if i not in given else
+            _arg(getattr(out, f), *shapes[i], dev, f) for i, f in enumerate(_ROUTING_FIELDS)]
+    if logits is not None:
+        ptrs[0] = pl
+        if out.logits is not logits:
+            out = replace(out, logits=logits)
+    _run("d2moe_route_scored", dev, stream, px, code, T, d, pw, pb, E, k, _SCORING[scoring],
+         None if select_bias is None else _arg(select_bias, (E,), f32, dev, "select_bias"), groups,
+         top_groups, int(renorm), scale,
+         None if token_req is None else _arg(token_req, (T,), i32, dev, "token_req"),
+         _arg(bit_table, (R, E), u8, dev, "bit_table"), R, b_min, b_max,
+         ctypes.byref(_Routing(*ptrs)))
+    return out
 
 
 # ---- forward ----------------------------------------------------------------

@@ -215,6 +215,33 @@ d2moe_status d2moe_route_learned(const void* x, d2moe_dtype x_dtype, int32_t T, 
                                        bit_logits, out, (hipStream_t)stream));
 }
 
+d2moe_status d2moe_route_scored(const void* x, d2moe_dtype x_dtype, int32_t T, int32_t d,
+                                const float* Wg, const float* bias, int32_t E, int32_t k,
+                                int32_t scoring, const float* select_bias, int32_t groups,
+                                int32_t top_groups, int32_t renorm, float scale,
+                                const int32_t* token_req, const uint8_t* bit_table, int32_t R,
+                                int32_t b_min, int32_t b_max, const d2moe_routing* out,
+                                void* stream) {
+  if (T < 0 || E < 1 || E > 64 || k < 1 || k > E || R < 1 || !ladder_ok(b_min, b_max))
+    return D2MOE_EINVAL;
+  if ((scoring != D2MOE_SOFTMAX && scoring != D2MOE_SIGMOID) || (renorm != 0 && renorm != 1) ||
+      !std::isfinite(scale) || groups < 1 || E % groups != 0 || top_groups < 1 ||
+      top_groups > groups || k > top_groups * (E / groups))
+    return D2MOE_EINVAL;
+  if (x && x_dtype != D2MOE_F32 && x_dtype != D2MOE_BF16) return D2MOE_EUNSUPPORTED;
+  if (x && (d < 1 || !Wg)) return D2MOE_EINVAL;
+  if (!out || !out->hist || !out->offsets || !out->expert_maxbit || !out->flags)
+    return D2MOE_EINVAL;
+  if (T > 0 && (!out->topk_idx || !out->topk_w || !out->topk_bits || !out->perm ||
+                !out->slot_of || !out->logits || !bit_table))
+    return D2MOE_EINVAL;
+  if ((long long)T * k > (1ll << 30)) return D2MOE_EINVAL;
+  return from_hip(launch_route_scored(x, x_dtype, T, d, Wg, bias, E, k, scoring == D2MOE_SIGMOID,
+                                      select_bias, groups, top_groups, renorm != 0, scale,
+                                      token_req, bit_table, R, b_min, b_max, out,
+                                      (hipStream_t)stream));
+}
+
 d2moe_status d2moe_moe_forward_workspace(int32_t T, int32_t d, int32_t d_ff, int32_t E,
                                          int32_t k, int32_t shared_d_ff, size_t* bytes) {
   if (T < 0 || d < 1 || d_ff < 1 || E < 1 || E > 64 || k < 1 || k > E || shared_d_ff < 0 ||

@@ -387,6 +387,12 @@ hipError_t run_gate(const XT* x, int T, int d, const float* Wg, const float* bia
 
 }  // namespace
 
+hipError_t launch_gate(const void* x, d2moe_dtype xd, int T, int d, const float* Wg,
+                       const float* bias, int E, float* logits, hipStream_t s) {
+  return xd == D2MOE_BF16 ? run_gate((const uint16_t*)x, T, d, Wg, bias, E, logits, s)
+                          : run_gate((const float*)x, T, d, Wg, bias, E, logits, s);
+}
+
 static hipError_t route_common(const void* x, d2moe_dtype xd, int T, int d, const float* Wg,
                                const float* bias, int E, int k, const BitSource& bs, int b_min,
                                int b_max, const d2moe_routing* out, hipStream_t s) {

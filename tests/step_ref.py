@@ -36,3 +36,50 @@ def rotate(x, err, cos, sin, pos, interleaved):
         np.abs(ea * c) + np.abs(eb * s) + 3 * U * (np.abs(a * c) + np.abs(b * s)),
         np.abs(eb * c) + np.abs(ea * s) + 3 * U * (np.abs(b * c) + np.abs(a * s)))
     return x, err
+
+
+# ---- routing by scores -----------------------------------------------------------------
+
+def route_scored(logits, k, token_req, table, scoring, select_bias, groups, top_groups, renorm,
+                 scale, b_min, b_max):
+    """The routing's tensors by name, one token after the other in binary64."""
+    T, E = logits.shape
+    L = b_max - b_min + 1
+    idx, w, bits = np.zeros((T, k), int), np.zeros((T, k)), np.zeros((T, k), int)
+    flags = 0
+    for t in range(T):
+        x = logits[t].astype(np.float64)
+        if scoring == "softmax":
+            top = np.max(x)
+            with np.errstate(invalid="ignore"):
+                e = np.where(x == top, 1.0, np.exp(x - top)) if top > -np.inf else np.zeros(E)
+            score = e / e.sum() if e.sum() > 0 else e
+        else:
+            with np.errstate(over="ignore"):
+                score = 1 / (1 + np.exp(-x))
+        by = score if select_bias is None else score + select_bias.astype(np.float64)
+        size = E // groups
+        value = [sum(sorted(by[g * size:(g + 1) * size])[-2:]) for g in range(groups)]
+        on = sorted(range(groups), key=lambda g: (-value[g], g))[:top_groups]
+        among = [e for e in range(E) if e // size in on]
+        sel = sorted(among, key=lambda e: (-by[e], e))[:k]
+        s = score[sel]
+        if renorm:
+            s = s / s.sum() if s.sum() > 0 else 0 * s
+        idx[t], w[t] = sel, s * scale
+        r = 0 if token_req is None else token_req[t]
+        if r < 0 or r >= len(table):
+            flags, r = flags | 2, min(max(r, 0), len(table) - 1)
+        b = table[r][sel].astype(int)
+        if ((b < b_min) | (b > b_max)).any():
+            flags |= 1
+        bits[t] = np.clip(b, b_min, b_max)
+    key = (idx * L + bits - b_min).reshape(-1)
+    hist = np.bincount(key, minlength=E * L).reshape(E, L)
+    perm = np.argsort(key, kind="stable")
+    slot = np.empty(T * k, int)
+    slot[perm] = np.arange(T * k)
+    most = [max([b_min + l for l in range(L) if hist[e, l]], default=0) for e in range(E)]
+    return dict(topk_idx=idx, topk_w=w, topk_bits=bits, hist=hist,
+                offsets=np.concatenate([[0], np.cumsum(hist.reshape(-1))]), perm=perm,
+                slot_of=slot, expert_maxbit=np.array(most), flags=np.array([flags]))

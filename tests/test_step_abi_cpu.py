@@ -41,3 +41,34 @@ def test_kv_append_norm_binding_refusals():
                dict(cos=t, sin=t)):                   # (the last: tensors on the host)
         with pytest.raises(ValueError):
             api.kv_append_norm(x, x, x, c, one[None], one, **kw)
+
+
+def routing():
+    return api._Routing(*([FAKE] * 10))
+
+
+def test_route_scored_refusals():
+    ok = dict(x=FAKE, xt=1, T=5, d=64, w=FAKE, b=None, E=16, k=4, sc=1, sb=None, g=4, tg=2, rn=1,
+              s=1.0, rq=None, bt=FAKE, R=2, lo=2, hi=8, o=routing(), st=None)
+    nan, inf = float("nan"), float("inf")
+    refuses("d2moe_route_scored", ok, [
+        dict(T=-1), dict(E=0), dict(E=65), dict(k=0), dict(k=17), dict(k=9), dict(sc=2),
+        dict(sc=-1), dict(g=0), dict(g=3), dict(g=-4), dict(g=32), dict(tg=0), dict(tg=5),
+        dict(rn=2), dict(s=nan), dict(s=inf), dict(R=0), dict(lo=0), dict(hi=9), dict(lo=5, hi=4),
+        dict(d=0), dict(w=None), dict(bt=None), dict(o=None), dict(T=1 << 29)])
+    for f, _ in api._Routing._fields_:
+        r = routing()
+        setattr(r, f, None)
+        refuses("d2moe_route_scored", ok, [dict(o=r), dict(o=r, x=None)])
+    refuses("d2moe_route_scored", ok, [dict(xt=2), dict(xt=-1)], api.EUNSUPPORTED)
+
+
+def test_route_scored_binding_refusals():
+    x, table = torch.zeros((3, 8)), torch.full((1, 8), 4, dtype=torch.uint8)
+    for kw in (dict(scoring="relu"), dict(x=x), dict(Wg=x), dict(select_bias=torch.zeros(7)),
+               dict(token_req=torch.zeros(3)), dict(out=api.Routing.empty(4, 8, 2, device="cpu")),
+               dict(logits=x.double()), dict(logits=None), dict(logits=None, x=x), dict(b_min=9),
+               dict(bit_table=table.int()), dict(bit_table=table[:, :7]), {}):
+        a = {**dict(logits=x, k=2, token_req=None, bit_table=table), **kw}
+        with pytest.raises(ValueError):       # (the last: tensors on the host)
+            api.route_scored(**a)
