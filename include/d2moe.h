@@ -657,6 +657,33 @@ d2moe_status d2moe_block_norm(float* x, float x_scale, const void* y, d2moe_dtyp
                               void* stream);
 
 /*
+ * A token for each of B rows of logits.  With w_i = exp((l_i - max l) / temperature) and
+ * the tokens in descending order of their logits, ties in ascending order of their
+ * indexes, the kept ones are the longest beginning of that order that
+ *   top_k    has top_k tokens at most (0 or less: no bound),
+ *   top_p    ends with the first token whose running sum reaches top_p times the sum of
+ *            what top_k leaves (1 or more: no bound; 0 or less: one token),
+ *   min_p    has w_i >= min_p throughout (0 or less: no bound; above 1 as 1),
+ * and the token is the first of them whose running sum exceeds u times their whole sum.
+ *   logits: device [B][V], rows `stride` elements apart
+ *   u: device [B] float, random numbers in [0, 1) (others count as the nearest of them)
+ *   temperature, top_p, min_p: device [B] float, top_k: device [B] int32, or NULL
+ *        (temperature 1; no bound); a NaN bound is none.  Temperature 0 or less, or
+ *        NaN: the first token of the order
+ *   tokens: device [B] int32; probs: device [B] float or NULL, the token's share of the
+ *        kept sum (1 with temperature 0)
+ * Tokens of logit -infinity or NaN are never chosen; a row of nothing else gives token
+ * -1 with share 0.  Logits of +infinity share the whole.  Weights are binary64, rounded
+ * to multiples of 2^-(62 - ceil(log2 V)) (2^-51 at most), whose sums are exact: the result
+ * does not depend on what else runs, and tokens of less than half a unit are not drawn.
+ * 1 <= V <= 2^24, B <= 2^24.
+ */
+d2moe_status d2moe_sample(const void* logits, d2moe_dtype dtype, int64_t stride, int32_t B,
+                          int32_t V, const float* u, const float* temperature,
+                          const int32_t* top_k, const float* top_p, const float* min_p,
+                          int32_t* tokens, float* probs, void* stream);
+
+/*
  * Measurement helper (not part of the layer): reads `bytes` of device memory
  * at `buf` once with 16-byte nontemporal loads in a grid-stride loop over
  * `blocks` workgroups of 256 threads and writes one XOR word per workgroup to

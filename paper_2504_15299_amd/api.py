@@ -117,7 +117,8 @@ def lib():
                                         size, _P]
         L.d2moe_block_norm.argtypes = [_P, f32, _P, _I, f32, _P, _P, _I, i64, _P, _I, _I, f32, _P,
                                        _I, _P]
-        for name in ("d2moe_linear_size", "d2moe_linear_pack", "d2moe_linear_pack_codes",
+        L.d2moe_sample.argtypes = [_P, _I, i64, _I, _I, _P, _P, _P, _P, _P, _P, _P, _P]
+        for name in ("d2moe_sample", "d2moe_linear_size", "d2moe_linear_pack", "d2moe_linear_pack_codes",
                      "d2moe_linear_forward", "d2moe_kv_append", "d2moe_kv_append_norm", "d2moe_attn_decode_workspace",
                      "d2moe_attn_decode", "d2moe_block_norm",
                      "d2moe_mwq_size", "d2moe_pack_mwq", "d2moe_debug_unpack", "d2moe_route",
@@ -786,6 +787,31 @@ def block_norm(x: torch.Tensor, y: torch.Tensor, eps: float = 1e-5, pre_weight=N
          gs, None if pre_weight is None else _arg(pre_weight, (d,), f32, dev, "pre_weight"), T, d,
          eps, ph, hd)
     return h
+
+
+def sample(logits: torch.Tensor, u: torch.Tensor, temperature=None, top_k=None, top_p=None,
+           min_p=None, tokens: torch.Tensor | None = None, probs: torch.Tensor | None = None,
+           stream=None):
+    """``d2moe_sample``: logits [B][V] float32 or bfloat16 (rows may be strided), u [B]
+    float32 in [0, 1); temperature, top_p, min_p [B] float32 and top_k [B] int32, each
+    or None.  Returns (tokens [B] int32, probs [B] float32)."""
+    (B, V), dev, f32, i32 = logits.shape, logits.get_device(), torch.float32, torch.int32
+    if logits.dtype not in _CODES:
+        raise TypeError(f"unsupported dtype {logits.dtype}")
+    if V > 1 and logits.stride(1) != 1:
+        raise ValueError("logits must have contiguous rows")
+    tokens = _new(u, (B,), i32, stream) if tokens is None else tokens
+    probs = _new(u, (B,), f32, stream) if probs is None else probs
+
+    def opt(t, dtype, what):
+        return None if t is None else _arg(t, (B,), dtype, dev, what)
+
+    _run("d2moe_sample", dev, stream, logits.data_ptr(), _CODES[logits.dtype],
+         logits.stride(0) if B > 1 else V, B, V, _arg(u, (B,), f32, dev, "u"),
+         opt(temperature, f32, "temperature"), opt(top_k, i32, "top_k"), opt(top_p, f32, "top_p"),
+         opt(min_p, f32, "min_p"), _arg(tokens, (B,), i32, dev, "tokens"),
+         _arg(probs, (B,), f32, dev, "probs"))
+    return tokens, probs
 
 
 def stream_read(buf: torch.Tensor, sink: torch.Tensor, stream=None) -> None:

@@ -500,6 +500,19 @@ d2moe_status d2moe_block_norm(float* x, float x_scale, const void* y, d2moe_dtyp
                                     (hipStream_t)stream));
 }
 
+d2moe_status d2moe_sample(const void* logits, d2moe_dtype dtype, int64_t stride, int32_t B,
+                          int32_t V, const float* u, const float* temperature,
+                          const int32_t* top_k, const float* top_p, const float* min_p,
+                          int32_t* tokens, float* probs, void* stream) {
+  if (!dtype_ok(dtype)) return D2MOE_EUNSUPPORTED;
+  if (B < 0 || B > (1 << 24) || V < 1 || V > (1 << 24) || (B > 1 && stride < V))
+    return D2MOE_EINVAL;
+  if (B > 0 && (!logits || !u || !tokens || !aligned(logits, (size_t)dtype_size(dtype))))
+    return D2MOE_EINVAL;
+  return from_hip(launch_sample(logits, dtype, stride, B, V, u, temperature, top_k, top_p, min_p,
+                                tokens, probs, (hipStream_t)stream));
+}
+
 d2moe_status d2moe_stream_read(const void* buf, size_t bytes, uint32_t* sink, int32_t blocks,
                                void* stream) {
   if (!buf || !sink || blocks < 1 || bytes % 16 != 0 || ((uintptr_t)buf & 15u) != 0)

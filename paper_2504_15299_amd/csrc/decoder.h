@@ -1,6 +1,6 @@
 // Internal declarations of the decode operators around the MoE layer: the
 // host-side launchers of linear.hip, linear_pack.hip, kv_append.hip,
-// attn_decode.hip and block_norm.hip.
+// attn_decode.hip, block_norm.hip and sample.hip.
 #pragma once
 
 #include "internal.h"
@@ -60,5 +60,10 @@ hipError_t launch_block_norm(float* x, float x_scale, const void* y, d2moe_dtype
                              const float* post_w, const void* gate, d2moe_dtype gd,
                              int64_t gate_stride, const float* pre_w, int T, int d, float eps,
                              void* h, d2moe_dtype hd, hipStream_t s);
+
+hipError_t launch_sample(const void* logits, d2moe_dtype dtype, int64_t stride, int B, int V,
+                         const float* u, const float* temperature, const int32_t* top_k,
+                         const float* top_p, const float* min_p, int32_t* tokens, float* probs,
+                         hipStream_t s);
 
 }  // namespace d2moe

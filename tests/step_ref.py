@@ -83,3 +83,37 @@ def route_scored(logits, k, token_req, table, scoring, select_bias, groups, top_
     return dict(topk_idx=idx, topk_w=w, topk_bits=bits, hist=hist,
                 offsets=np.concatenate([[0], np.cumsum(hist.reshape(-1))]), perm=perm,
                 slot_of=slot, expert_maxbit=np.array(most), flags=np.array([flags]))
+
+
+# ---- sampling ------------------------------------------------------------------------------
+
+def sample(l, u, t=1.0, k=0, p=1.0, m=0.0):
+    """(token, share, room) of one row: room is the least distance, in parts of the sums
+    concerned, of a choice to where it would turn."""
+    live = l > -np.inf
+    if not live.any():
+        return -1, 0.0, 1.0
+    order = np.argsort(np.where(live, -l.astype(np.float64), np.inf), kind="stable")[:live.sum()]
+    if not t > 0 or k == 1:
+        return int(order[0]), 1.0, 1.0
+    d = l[order].astype(np.float64)
+    with np.errstate(invalid="ignore"):
+        w = np.where(d == d[0], 1.0, np.exp((d - d[0]) / t))
+    w = np.where(w == w, w, 0.0)
+    if k > 0:
+        w = w[:k]
+    n, room = len(w), 1.0
+    if p < 1:
+        run = np.cumsum(w)
+        at = max(p, 0.0) * run[-1]
+        n = 1 + int((run[:-1] < at).sum())
+        room = min(room, np.abs(run - at).min() / run[-1]) if p > 0 else room
+    if m > 0:
+        n = min(n, int((w >= min(m, 1.0)).sum()))
+        room = min(room, np.abs(w[1:] - m).min()) if len(w) > 1 and m < 1 else room
+    run = np.cumsum(w[:n])
+    at = min(max(u, 0.0), 1.0) * run[-1]
+    i = min(int((run <= at).sum()), n - 1)
+    if u > 0:
+        room = min(room, np.abs(run - at).min() / run[-1])
+    return int(order[i]), w[i] / run[-1], room

@@ -72,3 +72,25 @@ def test_route_scored_binding_refusals():
         a = {**dict(logits=x, k=2, token_req=None, bit_table=table), **kw}
         with pytest.raises(ValueError):       # (the last: tensors on the host)
             api.route_scored(**a)
+
+
+def test_sample_refusals():
+    ok = dict(x=FAKE, xt=0, s=100, B=3, V=100, u=FAKE, t=None, k=None, p=None, m=None, o=FAKE,
+              pr=None, st=None)
+    refuses("d2moe_sample", ok, [dict(x=None), dict(u=None), dict(o=None), dict(B=-1),
+                                 dict(B=(1 << 24) + 1), dict(V=0), dict(V=-1), dict(s=99),
+                                 dict(V=(1 << 24) + 1, s=1 << 25), dict(x=FAKE + 2),
+                                 dict(x=FAKE + 1, xt=1)])
+    refuses("d2moe_sample", ok, [dict(xt=2), dict(xt=-1)], api.EUNSUPPORTED)
+    refuses("d2moe_sample", ok, [dict(B=0), dict(B=0, x=None, u=None, o=None)], api.OK)
+
+
+def test_sample_binding_refusals():
+    x, u = torch.zeros((3, 8)), torch.zeros(3)
+    for kw in (dict(u=u[:2]), dict(u=u.double()), dict(top_k=u), dict(top_p=u.half()),
+               dict(temperature=u[None]), dict(logits=x.t().contiguous().t()),
+               dict(tokens=u), dict(probs=u.int()), {}):
+        with pytest.raises(ValueError):       # (the last: tensors on the host)
+            api.sample(**{**dict(logits=x, u=u), **kw})
+    with pytest.raises(TypeError):
+        api.sample(x.half(), u)
