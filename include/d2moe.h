@@ -635,6 +635,38 @@ d2moe_status d2moe_attn_decode(const void* q, int64_t q_stride, int32_t B, int32
                                size_t ws_bytes, void* stream);
 
 /*
+ * d2moe_attn_decode where the sequences share a prefix, whose keys and values are read
+ * once for up to 64 queries of a key head.  Of sequence b's n = lengths[b] tokens the
+ * first s = min(prefix_lens[b], n) lie where the one row `prefix_table` says, the others
+ * where its own row of block_table says, at the same positions:
+ *     token p < s in page prefix_table[p / page_size],
+ *     token p >= s in page block_table[b][p / page_size],  both at p % page_size,
+ * so a prefix may end inside a page, a sequence may share less of it than others, or
+ * nothing (0), and a row's entries for pages that it shares are not looked at.
+ *   prefix_table: device [prefix_pages] int32; prefix_lens: device [B] int32, negative
+ *        ones count as 0, ones beyond the prefix's table as its end
+ *   max_prefix, max_rest: host, the largest s and n - s expected; only the division of
+ *        the work goes by them, any lengths give their result; at most 2^30
+ *   workspace: at least d2moe_attn_prefix_workspace bytes for these two (no fewer for
+ *        larger ones), 16-byte aligned; contents need no initialisation; calls that may
+ *        run at the same time need one each
+ *   out: packed; may begin where q does, whatever q's stride
+ * Everything else as d2moe_attn_decode without a window: lengths, masked tokens, rows
+ * without a key, types, sums and limits (also prefix_pages * page_size <= 2^30).  Value
+ * rows (not key rows) of tokens attended must be finite: an infinite one may give NaN.
+ */
+d2moe_status d2moe_attn_prefix_workspace(int32_t B, int32_t q_heads, int32_t n_heads,
+                                         int32_t head_dim, int32_t max_prefix, int32_t max_rest,
+                                         size_t* bytes);
+d2moe_status d2moe_attn_prefix(const void* q, int64_t q_stride, int32_t B, int32_t q_heads,
+                               const d2moe_kv_cache* cache, const int32_t* block_table,
+                               int32_t max_pages, const int32_t* lengths,
+                               const int32_t* prefix_table, int32_t prefix_pages,
+                               const int32_t* prefix_lens, int32_t max_prefix, int32_t max_rest,
+                               float scale, void* out, void* workspace, size_t ws_bytes,
+                               void* stream);
+
+/*
  * The norms after a block and before the next one, with the block's gate and
  * the residual's scales; d2moe_residual_rmsnorm with all of its parts:
  *     u    = post_w * y[t] / sqrt(mean_c y[t][c]^2 + eps)   (y[t] when

@@ -115,10 +115,13 @@ def lib():
         L.d2moe_attn_decode_workspace.argtypes = [_I, _I, _I, _I, _I, sz]
         L.d2moe_attn_decode.argtypes = [_P, i64, _I, _I, kvc, _P, _I, _P, _I, _I, f32, _P, _P,
                                         size, _P]
+        L.d2moe_attn_prefix_workspace.argtypes = [_I, _I, _I, _I, _I, _I, sz]
+        L.d2moe_attn_prefix.argtypes = [_P, i64, _I, _I, kvc, _P, _I, _P, _P, _I, _P, _I, _I, f32,
+                                        _P, _P, size, _P]
         L.d2moe_block_norm.argtypes = [_P, f32, _P, _I, f32, _P, _P, _I, i64, _P, _I, _I, f32, _P,
                                        _I, _P]
         L.d2moe_sample.argtypes = [_P, _I, i64, _I, _I, _P, _P, _P, _P, _P, _P, _P, _P]
-        for name in ("d2moe_sample", "d2moe_linear_size", "d2moe_linear_pack", "d2moe_linear_pack_codes",
+        for name in ("d2moe_sample", "d2moe_attn_prefix_workspace", "d2moe_attn_prefix", "d2moe_linear_size", "d2moe_linear_pack", "d2moe_linear_pack_codes",
                      "d2moe_linear_forward", "d2moe_kv_append", "d2moe_kv_append_norm", "d2moe_attn_decode_workspace",
                      "d2moe_attn_decode", "d2moe_block_norm",
                      "d2moe_mwq_size", "d2moe_pack_mwq", "d2moe_debug_unpack", "d2moe_route",
@@ -755,6 +758,53 @@ def attn_decode(q: torch.Tensor, cache: KVCache, block_table: torch.Tensor, leng
          _arg(block_table, (B, pages), torch.int32, dev, "block_table"), pages,
          _arg(lengths, (B,), torch.int32, dev, "lengths"), max_len, window,
          D ** -0.5 if scale is None else scale, po, pw, nw)
+    return out
+
+
+def attn_prefix_workspace(B: int, q_heads: int, cache: KVCache, max_prefix: int,
+                          max_rest: int) -> int:
+    n = ctypes.c_size_t()
+    _check("d2moe_attn_prefix_workspace",
+           lib().d2moe_attn_prefix_workspace(B, q_heads, cache.n_heads, cache.head_dim, max_prefix,
+                                             max_rest, ctypes.byref(n)))
+    return n.value
+
+
+def attn_prefix(q: torch.Tensor, cache: KVCache, block_table: torch.Tensor, lengths: torch.Tensor,
+                prefix_table: torch.Tensor, prefix_lens: torch.Tensor, scale: float | None = None,
+                max_prefix: int | None = None, max_rest: int | None = None,
+                out: torch.Tensor | None = None, workspace: torch.Tensor | None = None,
+                stream=None) -> torch.Tensor:
+    """``d2moe_attn_prefix``: attn_decode where sequence b's first prefix_lens[b] tokens
+    lie in the pages of prefix_table [prefix_pages], the others in those of its row of
+    block_table [B][max_pages]; prefix_lens [B] int32.  ``max_prefix`` and ``max_rest``,
+    the most tokens of either kind expected, are what the tables have room for when not
+    given."""
+    dev, dtype, D = cache.index, cache.k.dtype, cache.head_dim
+    B, heads = q.shape[:2]
+    shape, i32 = (B, heads, D), torch.int32
+    pq, qs = _rows(q, shape, dtype, dev, "q")
+    pages, head_pages = block_table.shape[1], prefix_table.shape[0]
+    if max_prefix is None:
+        max_prefix = min(head_pages * cache.page_size, 1 << 30)
+    if max_rest is None:
+        max_rest = min(pages * cache.page_size, 1 << 30)
+    if out is None:
+        out = _new(q, shape, dtype, stream)
+        po = out.data_ptr()
+    else:
+        po = _arg(out, shape, dtype, dev, "out")
+    if workspace is None:
+        need = attn_prefix_workspace(B, heads, cache, max_prefix, max_rest)
+        workspace = _new(q, (need,), torch.uint8, stream)
+    elif workspace.get_device() != dev or not workspace.is_contiguous():
+        raise ValueError(f"workspace must be a contiguous tensor on GPU {dev}")
+    _run("d2moe_attn_prefix", dev, stream, pq, qs, B, heads, cache._ref,
+         _arg(block_table, (B, pages), i32, dev, "block_table"), pages,
+         _arg(lengths, (B,), i32, dev, "lengths"),
+         _arg(prefix_table, (head_pages,), i32, dev, "prefix_table"), head_pages,
+         _arg(prefix_lens, (B,), i32, dev, "prefix_lens"), max_prefix, max_rest,
+         D ** -0.5 if scale is None else scale, po, workspace.data_ptr(), workspace.nbytes)
     return out
 
 

@@ -484,6 +484,48 @@ d2moe_status d2moe_attn_decode(const void* q, int64_t q_stride, int32_t B, int32
                                      (hipStream_t)stream));
 }
 
+static bool prefix_shape_ok(int B, int q_heads, int n_heads, int dim, int max_prefix,
+                            int max_rest) {
+  return max_prefix <= (1 << 30) && max_rest <= (1 << 30) &&
+         attn_shape_ok(B, q_heads, n_heads, dim, max_prefix) && max_rest >= 0;
+}
+
+d2moe_status d2moe_attn_prefix_workspace(int32_t B, int32_t q_heads, int32_t n_heads,
+                                         int32_t head_dim, int32_t max_prefix, int32_t max_rest,
+                                         size_t* bytes) {
+  if (!prefix_shape_ok(B, q_heads, n_heads, head_dim, max_prefix, max_rest) || !bytes)
+    return D2MOE_EINVAL;
+  *bytes = attn_prefix_workspace(B, q_heads, n_heads, head_dim, max_prefix, max_rest);
+  return D2MOE_OK;
+}
+
+d2moe_status d2moe_attn_prefix(const void* q, int64_t q_stride, int32_t B, int32_t q_heads,
+                               const d2moe_kv_cache* cache, const int32_t* block_table,
+                               int32_t max_pages, const int32_t* lengths,
+                               const int32_t* prefix_table, int32_t prefix_pages,
+                               const int32_t* prefix_lens, int32_t max_prefix, int32_t max_rest,
+                               float scale, void* out, void* workspace, size_t ws_bytes,
+                               void* stream) {
+  if (!cache_ok(cache) ||
+      !prefix_shape_ok(B, q_heads, cache->n_heads, cache->head_dim, max_prefix, max_rest) ||
+      max_pages < 0 || prefix_pages < 0 || !std::isfinite(scale * kLog2e) ||
+      (int64_t)max_pages * cache->page_size > (1 << 30) ||
+      (int64_t)prefix_pages * cache->page_size > (1 << 30))
+    return D2MOE_EINVAL;
+  if (B == 0) return D2MOE_OK;
+  const int64_t step = 16 / dtype_size(cache->dtype);
+  if (!q || !out || !lengths || !prefix_lens || !aligned(q, 16) || !aligned(out, 16) ||
+      q_stride % step != 0 || (B > 1 && q_stride < (int64_t)q_heads * cache->head_dim) ||
+      (max_pages > 0 && !block_table) || (prefix_pages > 0 && !prefix_table))
+    return D2MOE_EINVAL;
+  const size_t need =
+      attn_prefix_workspace(B, q_heads, cache->n_heads, cache->head_dim, max_prefix, max_rest);
+  if (!workspace || ws_bytes < need || !aligned(workspace, 16)) return D2MOE_EWORKSPACE;
+  return from_hip(launch_attn_prefix(q, q_stride, B, q_heads, cache, block_table, max_pages,
+                                     lengths, prefix_table, prefix_pages, prefix_lens, max_prefix,
+                                     max_rest, scale, out, workspace, (hipStream_t)stream));
+}
+
 d2moe_status d2moe_block_norm(float* x, float x_scale, const void* y, d2moe_dtype y_dtype,
                               float y_scale, const float* post_w, const void* gate,
                               d2moe_dtype gate_dtype, int64_t gate_stride, const float* pre_w,

@@ -20,14 +20,10 @@
 // Bound by reading the cache: 4 len head_dim bytes (bf16) per key head against
 // 16-column products that keep the matrix units busy for a twelfth of the time (64
 // sequences of 8192 keys).
-#include "decoder.h"
+#include "attn_tile.h"
 
 namespace d2moe {
 namespace {
-
-typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
-typedef float f4 __attribute__((ext_vector_type(4)));
-typedef uint32_t u4 __attribute__((ext_vector_type(4)));
 
 constexpr int kHeadTile = 16;    // query heads of a workgroup
 constexpr int kChunk = 512;      // keys whose row offsets are worked out at a time
@@ -111,20 +107,6 @@ __device__ inline int row_share(const Row& r, int per, int groups) {
   return share > kMinShare ? share : kMinShare;
 }
 
-__device__ inline float fast_exp2(float x) { return __builtin_amdgcn_exp2f(x); }
-
-__device__ inline f4 mma(u4 a, u4 b, f4 c) {
-  f4 d = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a),
-                                                 __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
-  asm("" : "+v"(d) : "v"(a), "v"(b));  // the result gets registers of its own
-  return d;
-}
-__device__ inline f4 mma(float a, float b, f4 c) {
-  f4 d = __builtin_amdgcn_mfma_f32_16x16x4f32(a, b, c, 0, 0, 0);
-  asm("" : "+v"(d) : "v"(a), "v"(b));
-  return d;
-}
-
 // The tile products of one cache type: TK keys a step, a lane's share of the key
 // rows as loaded (K), of the value rows (V) and of Q.  Head dimensions past D, where
 // it is below DP (PAD), are zero in K and Q; value loads past D read the row's
@@ -140,11 +122,6 @@ __device__ inline f4 mma(float a, float b, f4 c) {
 // Of a value row a lane loads VE consecutive values, dimensions 16 VE h + VE (l % 16)
 // + 0 .. VE - 1, so that 16 lanes read a run of 16 VE values; element i of that run
 // is the row l % 16 of value product (h, i).
-template <int CPR>
-__device__ inline int swizzle(int row) {
-  return CPR >= 16 ? row & 15 : (row >> 1) & 7;
-}
-
 template <typename E, int DP, int TK_>
 struct KeyRows {
   static constexpr int TK = TK_, PER = 16 / sizeof(E), CPR = DP / PER;
@@ -353,30 +330,6 @@ struct Tile<float, DP, PAD> : KeyRows<float, DP, 16> {
         for (int j = 0; j < NV; ++j) o[h][i] = mma(v.f[j][h][i], p[j], o[h][i]);
   }
 };
-
-// A barrier for LDS alone: a full one would also wait for the loads under way.
-__device__ inline void lds_barrier() {
-  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
-  __builtin_amdgcn_s_barrier();
-  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
-}
-
-// LDS between the lanes of a wave.
-__device__ inline void wave_handoff() {
-  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-  __builtin_amdgcn_wave_barrier();
-  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
-}
-
-// Four values of a result row.
-template <typename T>
-__device__ inline void store4(T* p, f4 v) {
-  if constexpr (sizeof(T) == 2)
-    *(uint2*)p = make_uint2(f2bf(v[0]) | (uint32_t)f2bf(v[1]) << 16,
-                            f2bf(v[2]) | (uint32_t)f2bf(v[3]) << 16);
-  else
-    *(f4*)p = v;
-}
 
 // WAVES waves take tiles of TK keys in turn; HT: query heads that the workgroup
 // may have (4 or 16; columns past them are computed on zeros).  SPLIT: a

@@ -1,0 +1,600 @@
+// Attention of one new token per sequence where the sequences share a prefix:
+//   out[b][h] = sum_j softmax_j(scale q[b][h] . K_j) V_j,
+// j over the shared tokens (one block table for all) and then the sequence's own.
+//
+// The queries of all sequences and of one key head are the rows of one product with
+// the prefix's keys, up to 64 at a time, so that a shared key is read once for 64
+// queries.  A workgroup takes a run of keys for its rows, of the prefix or of one
+// sequence's own tokens, keeps the running maximum m, sum l of exp2(score - m) and
+// value sum O, and leaves them as a part in the workspace; a second kernel joins the
+// parts of each query.  Both kinds of run are in one launch: the prefix's are bound by
+// the matrix units, the own tokens' by memory.
+//
+// As in the attention of single sequences,
+//   S (keys x queries) = K Q^T,   O^T (values x queries) = V^T P^T
+// leave one query in lane column l % 16, and the second product takes its keys in the
+// order in which the first left them: no exchange between the products.
+#include "attn_tile.h"
+
+namespace d2moe {
+namespace {
+
+constexpr int kThreads = 256, kWaves = 4;
+constexpr int kRows = 16;  // queries of a lane column set
+
+struct PrefixArgs {
+  const void *q, *k, *v;
+  int64_t q_stride, page_stride, token_stride, head_stride;
+  const int32_t *table, *lengths, *prefix_table, *prefix_lens;
+  FastDiv page;
+  int B, n_pages, max_pages, prefix_pages, Hq, H, G, D;
+  float scale_log2;  // scale / ln 2
+  int row_tiles, splits, chunk;           // of the prefix: row tiles, runs of `chunk` keys
+  int head_tiles, own_splits, own_chunk;  // of a sequence's own tokens
+  int shared_groups, own_groups;
+  float *shared_o, *shared_ml, *own_o, *own_ml;  // parts: rows of D and of (m, l)
+  void* out;
+};
+
+// Tokens of sequence b that lie in the prefix, and the end of its own.
+__device__ inline int shared_end(const PrefixArgs& a, int b) {
+  const int64_t room = (int64_t)a.prefix_pages * a.page.d;
+  int p = a.prefix_lens[b];
+  const int n = a.lengths[b];
+  p = p < n ? p : n;
+  return p < 0 ? 0 : p > room ? (int)room : p;
+}
+__device__ inline int own_end(const PrefixArgs& a, int b) {
+  const int64_t room = (int64_t)a.max_pages * a.page.d;
+  const int n = a.lengths[b];
+  return n < 0 ? 0 : n > room ? (int)room : n;
+}
+
+// The products of a wave: TK keys with 16 queries a column set.  K and V lie in LDS as
+// rows of CPR chunks of 16 bytes, K's swizzled.  Of a value row a lane takes VE
+// consecutive values, 16 lanes a run of 16 VE; element i of run h is row l % 16 of value
+// product (h, i).
+template <typename T, int DP>
+struct Products;
+
+template <int DP>
+struct Products<uint16_t, DP> {
+  static constexpr int TK = 32, PER = 8, CPR = DP / PER, KS = CPR / 4;
+  static constexpr int VE = DP >= 128 ? 8 : 4, H = DP / (16 * VE), NS = 8;
+  struct Q { u4 f[KS]; };
+  __device__ static int key_of(int j, int q) { return j < 4 ? 4 * q + j : 12 + 4 * q + j; }
+  __device__ static void load_q(Q& o, const uint16_t* row, int q, int D) {
+#pragma unroll
+    for (int s = 0; s < KS; ++s) {
+      const int c = 32 * s + 8 * q;
+      o.f[s] = row && c < D ? *(const u4*)(row + c) : u4{0, 0, 0, 0};
+    }
+  }
+  template <int CT>
+  __device__ static void scores(f4 (&s)[CT][2], const u4* k, const Q (&q)[CT], int lane) {
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      u4 x[KS];
+      const int row = 16 * t + (lane & 15);
+#pragma unroll
+      for (int c = 0; c < KS; ++c) x[c] = k[row * CPR + ((4 * c + (lane >> 4)) ^ swizzle<CPR>(row))];
+#pragma unroll
+      for (int ct = 0; ct < CT; ++ct) {
+        s[ct][t] = f4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+        for (int c = 0; c < KS; ++c) s[ct][t] = mma(x[c], q[ct].f[c], s[ct][t]);
+      }
+    }
+  }
+  // p as three bf16 pieces whose sum is exact: each is what is left, rounded, and leaves
+  // eight bits less.
+  struct P { u4 piece[3]; };
+  __device__ static void split(P& o, const float (&p)[NS]) {
+#pragma unroll
+    for (int d = 0; d < 4; ++d) {
+      float a = p[2 * d], b = p[2 * d + 1];
+#pragma unroll
+      for (int k = 0; k < 3; ++k) {
+        const uint32_t both = pack(a, b);
+        o.piece[k][d] = both;
+        if (k < 2) {
+          a -= __uint_as_float(both << 16);
+          b -= __uint_as_float(both & 0xffff0000u);
+        }
+      }
+    }
+  }
+  __device__ static uint32_t pack(float a, float b) {  // to nearest even
+    typedef float f2 __attribute__((ext_vector_type(2)));
+    typedef __bf16 b2 __attribute__((ext_vector_type(2)));
+    return __builtin_bit_cast(uint32_t, __builtin_convertvector((f2{a, b}), b2));
+  }
+  template <int CT>
+  __device__ static void values(f4 (&o)[CT][H][VE], const P (&p)[CT], const u4* v, int lane) {
+    const int q = lane >> 4;
+#pragma unroll
+    for (int h = 0; h < H; ++h) {
+      uint32_t x[NS][VE / 2];
+#pragma unroll
+      for (int j = 0; j < NS; ++j) {
+        const u4* row = v + key_of(j, q) * CPR;
+        if constexpr (VE == 8) {
+          const u4 w = row[16 * h + (lane & 15)];
+#pragma unroll
+          for (int d = 0; d < 4; ++d) x[j][d] = w[d];
+        } else {
+          const uint2 w = *((const uint2*)row + 16 * h + (lane & 15));
+          x[j][0] = w.x, x[j][1] = w.y;
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < VE; ++i) {
+        u4 a;
+#pragma unroll
+        for (int d = 0; d < 4; ++d)
+          a[d] = __builtin_amdgcn_perm(x[2 * d + 1][i / 2], x[2 * d][i / 2],
+                                       (i & 1) ? 0x07060302u : 0x05040100u);
+#pragma unroll
+        for (int k = 0; k < 3; ++k)
+#pragma unroll
+          for (int ct = 0; ct < CT; ++ct) o[ct][h][i] = mma(a, p[ct].piece[k], o[ct][h][i]);
+      }
+    }
+  }
+};
+
+template <int DP>
+struct Products<float, DP> {
+  static constexpr int TK = 16, PER = 4, CPR = DP / PER, KS = CPR / 4;
+  static constexpr int VE = 4, H = DP / 64, NS = 4;
+  struct Q { f4 f[KS]; };
+  __device__ static int key_of(int j, int q) { return 4 * q + j; }
+  __device__ static void load_q(Q& o, const float* row, int q, int D) {
+#pragma unroll
+    for (int s = 0; s < KS; ++s) {
+      const int c = 16 * s + 4 * q;
+      o.f[s] = row && c < D ? *(const f4*)(row + c) : f4{0.0f, 0.0f, 0.0f, 0.0f};
+    }
+  }
+  template <int CT>
+  __device__ static void scores(f4 (&s)[CT][1], const u4* k, const Q (&q)[CT], int lane) {
+#pragma unroll
+    for (int ct = 0; ct < CT; ++ct) s[ct][0] = f4{0.0f, 0.0f, 0.0f, 0.0f};
+    const int row = lane & 15;
+#pragma unroll
+    for (int c = 0; c < KS; ++c) {
+      const f4 x = __builtin_bit_cast(f4, k[row * CPR + ((4 * c + (lane >> 4)) ^ swizzle<CPR>(row))]);
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+#pragma unroll
+        for (int ct = 0; ct < CT; ++ct) {
+          const f4 acc = s[ct][0];
+          s[ct][0] = mma(x[e], q[ct].f[c][e], acc);
+          // nor shares part of its registers with the sum so far
+          if (c + e > 0) asm("" : "+v"(s[ct][0]) : "v"(acc));
+        }
+    }
+  }
+  struct P { float p[NS]; };
+  __device__ static void split(P& o, const float (&p)[NS]) {
+#pragma unroll
+    for (int j = 0; j < NS; ++j) o.p[j] = p[j];
+  }
+  template <int CT>
+  __device__ static void values(f4 (&o)[CT][H][VE], const P (&p)[CT], const u4* v, int lane) {
+    const int q = lane >> 4;
+#pragma unroll
+    for (int h = 0; h < H; ++h)
+#pragma unroll
+      for (int j = 0; j < NS; ++j) {
+        const f4 x = __builtin_bit_cast(f4, v[key_of(j, q) * CPR + 16 * h + (lane & 15)]);
+#pragma unroll
+        for (int i = 0; i < VE; ++i)
+#pragma unroll
+          for (int ct = 0; ct < CT; ++ct) o[ct][h][i] = mma(x[i], p[ct].p[j], o[ct][h][i]);
+      }
+  }
+};
+
+// A run's division among the waves: NC of them share a tile of keys, CT column sets
+// each, the others (kWaves / NC key groups) take other tiles of the same step.
+template <typename T, int DP, int CT, int NC>
+struct Run {
+  using M = Products<T, DP>;
+  static constexpr int NG = kWaves / NC, KEYS = NG * M::TK, ROWS = 16 * CT * NC;
+  static constexpr int EACH = KEYS * M::CPR / kThreads;  // chunks of K, and of V, a thread
+  static_assert(KEYS * M::CPR % kThreads == 0, "whole chunks");
+  struct Step {
+    u4 k[KEYS * M::CPR], v[KEYS * M::CPR];
+    float none[KEYS];  // 0, or -infinity where there is no key
+  };
+  struct Join {
+    float m[NG][ROWS], l[NG][ROWS];
+    __align__(16) float o[NG][ROWS][DP + 4];
+  };
+  union Lds {
+    Step step;
+    Join join;
+  };
+};
+
+// Keys k0 .. k1 - 1 of `table` (pages of it) and key head hk for the rows of a tile:
+// row(r) is query r, or null; limit(r) the end of the keys that it attends.  Rows 0 ..
+// rows - 1 go to part_o and part_ml.
+template <typename T, int DP, int CT, int NC, typename RowOf, typename LimitOf>
+__device__ void attend(const PrefixArgs& a, typename Run<T, DP, CT, NC>::Lds& lds,
+                       const int32_t* table, int pages, int hk, int k0, int k1, RowOf row_of,
+                       LimitOf limit_of, int rows, float* part_o, float* part_ml) {
+  using R = Run<T, DP, CT, NC>;
+  using M = typename R::M;
+  constexpr int CPR = M::CPR, PER = M::PER, EACH = R::EACH;
+  const int tid = threadIdx.x, lane = tid & 63, col = lane & 15, q = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), kg = wave / NC, cg = wave % NC;
+  if (k1 <= k0) {
+    if (tid < rows) *(float2*)(part_ml + 2 * tid) = make_float2(-INFINITY, 0.0f);
+    return;
+  }
+  const T* kc = (const T*)a.k + hk * a.head_stride;
+  const T* vc = (const T*)a.v + hk * a.head_stride;
+  typename M::Q qf[CT];
+  int limit[CT], least = 0x7fffffff;
+#pragma unroll
+  for (int ct = 0; ct < CT; ++ct) {
+    const int r = (cg * CT + ct) * 16 + col;
+    M::load_q(qf[ct], (const T*)row_of(r), q, a.D);
+    limit[ct] = limit_of(r);
+    least = limit[ct] < least ? limit[ct] : least;
+  }
+  float m[CT], l[CT];
+  f4 o[CT][M::H][M::VE];
+#pragma unroll
+  for (int ct = 0; ct < CT; ++ct) {
+    m[ct] = -INFINITY, l[ct] = 0.0f;
+#pragma unroll
+    for (int h = 0; h < M::H; ++h)
+#pragma unroll
+      for (int i = 0; i < M::VE; ++i) o[ct][h][i] = f4{0.0f, 0.0f, 0.0f, 0.0f};
+  }
+
+  // chunk e of this thread: row (e kThreads + tid) / CPR of the step, chunk tid % CPR
+  const int c = tid % CPR;
+  const bool wide = c * PER < a.D;
+  int page[EACH];
+  u4 kf[EACH], vf[EACH];
+  uint32_t have = 0;
+  auto fetch = [&](int s) {  // the pages of step s
+#pragma unroll
+    for (int e = 0; e < EACH; ++e) {
+      const uint32_t key = k0 + s * R::KEYS + (e * kThreads + tid) / CPR;
+      const uint32_t at = a.page.div(key);
+      page[e] = table[at < (uint32_t)pages ? at : (uint32_t)pages - 1];
+    }
+  };
+  auto load = [&](int s) {  // and their rows: whatever row where there is no key
+    have = 0;
+#pragma unroll
+    for (int e = 0; e < EACH; ++e) {
+      const uint32_t key = k0 + s * R::KEYS + (e * kThreads + tid) / CPR;
+      const bool in = key < (uint32_t)k1 && (uint32_t)page[e] < (uint32_t)a.n_pages;
+      const int64_t at = in ? page[e] * a.page_stride +
+                                  (int64_t)(key - a.page.div(key) * a.page.d) * a.token_stride
+                            : 0;
+      const int d = wide ? c * PER : 0;
+      kf[e] = *(const u4*)(kc + at + d);
+      vf[e] = *(const u4*)(vc + at + d);
+      have |= (in ? 1u : 0u) << e;
+    }
+  };
+  const int steps = (k1 - k0 + R::KEYS - 1) / R::KEYS;
+  fetch(0);
+  load(0);
+  if (steps > 1) fetch(1);
+  for (int s = 0; s < steps; ++s) {
+    lds_barrier();  // the step before has been used
+#pragma unroll
+    for (int e = 0; e < EACH; ++e) {
+      const int row = (e * kThreads + tid) / CPR;
+      const bool in = have >> e & 1, live = in && wide;
+      const u4 zero = {0, 0, 0, 0};  // not what a masked row holds: 0 times it is not 0
+      lds.step.k[row * CPR + (c ^ swizzle<CPR>(row))] = live ? kf[e] : zero;
+      lds.step.v[row * CPR + c] = live ? vf[e] : zero;
+      if (c == 0) lds.step.none[row] = in ? 0.0f : -INFINITY;
+    }
+    lds_barrier();
+    if (s + 1 < steps) load(s + 1);
+    if (s + 2 < steps) fetch(s + 2);
+
+    f4 sc[CT][M::NS / 4];
+    M::scores(sc, lds.step.k + kg * M::TK * CPR, qf, lane);
+    const int first = k0 + s * R::KEYS + kg * M::TK;
+    const bool border = __any(first + M::TK > least);
+    typename M::P p[CT];
+#pragma unroll
+    for (int ct = 0; ct < CT; ++ct) {
+      float x[M::NS], mx = -INFINITY;
+#pragma unroll
+      for (int t = 0; t < M::NS / 4; ++t) {
+        const f4 none = *(const f4*)&lds.step.none[kg * M::TK + 16 * t + 4 * q];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int j = 4 * t + i;
+          x[j] = fmaf(sc[ct][t][i], a.scale_log2, none[i]);
+          if (border && first + M::key_of(j, q) >= limit[ct]) x[j] = -INFINITY;
+          mx = fmaxf(mx, x[j]);
+        }
+      }
+      mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
+      mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
+      const float m_new = fmaxf(m[ct], mx);
+      const float ref = m_new == -INFINITY ? 0.0f : m_new;  // nothing but masked keys so far
+      const float alpha = fast_exp2(m[ct] - ref);
+      m[ct] = m_new;
+      l[ct] *= alpha;
+#pragma unroll
+      for (int j = 0; j < M::NS; ++j) {
+        x[j] = fast_exp2(x[j] - ref);
+        l[ct] += x[j];
+      }
+      if (__any(alpha != 1.0f)) {
+#pragma unroll
+        for (int h = 0; h < M::H; ++h)
+#pragma unroll
+          for (int i = 0; i < M::VE; ++i) o[ct][h][i] *= alpha;
+      }
+      M::split(p[ct], x);
+    }
+    M::values(o, p, lds.step.v + kg * M::TK * CPR, lane);
+  }
+
+  // join the key groups: every row's m, l and O
+  lds_barrier();
+#pragma unroll
+  for (int ct = 0; ct < CT; ++ct) {
+    const int r = (cg * CT + ct) * 16 + col;
+    l[ct] += __shfl_xor(l[ct], 16, 64);
+    l[ct] += __shfl_xor(l[ct], 32, 64);
+    if (q == 0) {
+      lds.join.m[kg][r] = m[ct];
+      lds.join.l[kg][r] = l[ct];
+    }
+#pragma unroll
+    for (int h = 0; h < M::H; ++h)
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+#pragma unroll
+        for (int i = 0; i < M::VE; i += 4)
+          *(f4*)&lds.join.o[kg][r][16 * M::VE * h + M::VE * (4 * q + e) + i] =
+              f4{o[ct][h][i][e], o[ct][h][i + 1][e], o[ct][h][i + 2][e], o[ct][h][i + 3][e]};
+  }
+  lds_barrier();
+  const int row4 = a.D / 4;
+  for (int i = tid; i < rows * row4; i += kThreads) {
+    const int r = i / row4, d = (i - r * row4) * 4;
+    float mm = -INFINITY, ll = 0.0f;
+    f4 acc = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+    for (int g = 0; g < R::NG; ++g) mm = fmaxf(mm, lds.join.m[g][r]);
+    const float ref = mm == -INFINITY ? 0.0f : mm;
+#pragma unroll
+    for (int g = 0; g < R::NG; ++g) {
+      const float f = fast_exp2(lds.join.m[g][r] - ref);
+      ll = fmaf(f, lds.join.l[g][r], ll);
+      acc += f * *(const f4*)&lds.join.o[g][r][d];
+    }
+    *(f4*)(part_o + (int64_t)r * a.D + d) = acc;
+    if (d == 0) *(float2*)(part_ml + 2 * r) = make_float2(mm, ll);
+  }
+}
+
+// Row tiles of the prefix, 16 CT NC rows each: query r of a key head is head r % G of
+// sequence r / G.
+template <typename T, int DP, int CT, int NC>
+__device__ void attend_shared(const PrefixArgs& a, typename Run<T, DP, CT, NC>::Lds& lds, int u) {
+  constexpr int ROWS = Run<T, DP, CT, NC>::ROWS;
+  const int hk = u % a.H, tile = u / a.H % a.row_tiles, split = u / a.H / a.row_tiles;
+  const int r0 = tile * ROWS, total = a.B * a.G, rows = total - r0 < ROWS ? total - r0 : ROWS;
+  // the end of the keys that any row attends
+  __shared__ int last;
+  if (threadIdx.x == 0) last = 0;
+  __syncthreads();
+  if ((int)threadIdx.x < rows) atomicMax(&last, shared_end(a, (r0 + threadIdx.x) / a.G));
+  __syncthreads();
+  const int k0 = split * a.chunk;
+  const int end = last, k1 = split + 1 < a.splits && k0 + a.chunk < end ? k0 + a.chunk : end;
+  const int64_t part = (int64_t)u * ROWS;
+  attend<T, DP, CT, NC>(
+      a, lds, a.prefix_table, a.prefix_pages, hk, k0, k1,
+      [&](int r) -> const T* {
+        if (r >= rows) return nullptr;
+        const int b = (r0 + r) / a.G, g = r0 + r - b * a.G;
+        return (const T*)a.q + b * a.q_stride + (int64_t)(hk * a.G + g) * a.D;
+      },
+      [&](int r) { return r < rows ? shared_end(a, (r0 + r) / a.G) : 0x7fffffff; }, rows,
+      a.shared_o + part * a.D, a.shared_ml + part * 2);
+}
+
+// A sequence's own tokens, 16 query heads of a key head at a time.
+template <typename T, int DP>
+__device__ void attend_own(const PrefixArgs& a, typename Run<T, DP, 1, 1>::Lds& lds, int u) {
+  const int hk = u % a.H, tile = u / a.H % a.head_tiles;
+  const int b = u / a.H / a.head_tiles % a.B, split = u / a.H / a.head_tiles / a.B;
+  const int g0 = tile * kRows, rows = a.G - g0 < kRows ? a.G - g0 : kRows;
+  const int from = shared_end(a, b), end = own_end(a, b);
+  const int64_t k0 = from + (int64_t)split * a.own_chunk;
+  const int k1 = split + 1 < a.own_splits && k0 + a.own_chunk < end ? (int)k0 + a.own_chunk : end;
+  const int64_t part = (int64_t)u * (a.G < kRows ? a.G : kRows);
+  attend<T, DP, 1, 1>(
+      a, lds, a.table + (int64_t)b * a.max_pages, a.max_pages, hk,
+      k0 < 0x7fffffff ? (int)k0 : 0x7fffffff, k1,
+      [&](int r) -> const T* {
+        return r < rows ? (const T*)a.q + b * a.q_stride + (int64_t)(hk * a.G + g0 + r) * a.D
+                        : nullptr;
+      },
+      [&](int) { return 0x7fffffff; }, rows, a.own_o + part * a.D, a.own_ml + part * 2);
+}
+
+// Both kinds of workgroups in turns of eight (one on each die).
+template <typename T, int DP, int CT, int NC>
+__global__ __launch_bounds__(kThreads, DP <= 128 ? 2 : 1) void attn_prefix_kernel(PrefixArgs a) {
+  union Lds {
+    typename Run<T, DP, CT, NC>::Lds shared;
+    typename Run<T, DP, 1, 1>::Lds own;
+  };
+  __shared__ Lds lds;
+  const int i = blockIdx.x;
+  const int both =
+      (a.shared_groups < a.own_groups ? a.shared_groups : a.own_groups) / 8 * 8;
+  int u = i / 16 * 8 + i % 8;
+  bool shared = i % 16 < 8;
+  if (i >= 2 * both) {
+    u = i - both;
+    shared = u < a.shared_groups;
+    if (!shared) u = u - a.shared_groups + both;
+  }
+  if (shared)
+    attend_shared<T, DP, CT, NC>(a, lds.shared, u);
+  else
+    attend_own<T, DP>(a, lds.own, u);
+}
+
+// Joins the parts of a query, one wave each: the prefix's runs, then its own.  Half waves
+// take parts in turn where a row has no more than 128 values.
+template <typename T>
+__global__ __launch_bounds__(kThreads) void attn_prefix_join_kernel(PrefixArgs a, int tile_rows) {
+  const int64_t row = (int64_t)blockIdx.x * kWaves + (threadIdx.x >> 6);
+  if (row >= (int64_t)a.B * a.Hq) return;
+  const int b = (int)(row / a.Hq), head = (int)(row - (int64_t)b * a.Hq);
+  const int hk = head / a.G, g = head - hk * a.G, lane = threadIdx.x & 63;
+  const int wide = a.D <= 128 ? 32 : 64, lanes = 64 / wide, sub = lane / wide;
+  const int d = 4 * (lane % wide), own_rows = a.G < kRows ? a.G : kRows;
+  const int r = b * a.G + g, tile = r / tile_rows, n = a.splits + a.own_splits;
+  float mm = -INFINITY, ll = 0.0f;
+  f4 acc = {0.0f, 0.0f, 0.0f, 0.0f};
+  for (int i = sub; i < n; i += lanes) {
+    const float *po, *pm;
+    if (i < a.splits) {
+      const int64_t p = (((int64_t)i * a.row_tiles + tile) * a.H + hk) * tile_rows + r % tile_rows;
+      po = a.shared_o + p * a.D, pm = a.shared_ml + p * 2;
+    } else {
+      const int64_t u = (((int64_t)(i - a.splits) * a.B + b) * a.head_tiles + g / kRows) * a.H + hk;
+      const int64_t p = u * own_rows + g % kRows;
+      po = a.own_o + p * a.D, pm = a.own_ml + p * 2;
+    }
+    const float2 ml = *(const float2*)pm;
+    if (ml.x == -INFINITY) continue;  // no key of it, and maybe no values written
+    const f4 v = d < a.D ? *(const f4*)(po + d) : f4{0.0f, 0.0f, 0.0f, 0.0f};
+    const float top = fmaxf(mm, ml.x), was = fast_exp2(mm - top), f = fast_exp2(ml.x - top);
+    mm = top;
+    ll = fmaf(f, ml.y, ll * was);
+    acc = acc * was + f * v;
+  }
+  if (lanes == 2) {
+    const float other = __shfl_xor(mm, 32, 64), top = fmaxf(mm, other);
+    const float f = fast_exp2(mm - (top == -INFINITY ? 0.0f : top));
+    ll *= f;
+    acc *= f;
+    ll += __shfl_xor(ll, 32, 64);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) acc[e] += __shfl_xor(acc[e], 32, 64);
+  }
+  if (sub == 0 && d < a.D)
+    store4((T*)a.out + row * a.D + d, acc * (ll == 0.0f ? 0.0f : 1.0f / ll));
+}
+
+// How a call is divided, from the sizes alone.
+struct Plan {
+  int tile_rows, row_tiles, splits, chunk, head_tiles, own_splits, own_chunk;
+};
+constexpr int kGroups = 512;     // of each kind, two a CU
+constexpr int kLeastKeys = 128;  // of a run
+constexpr int kMostSplits = 64;
+
+void divide(int keys, int64_t units, int& splits, int& chunk) {
+  int64_t most = units >= kGroups ? 1 : kGroups / units;
+  most = most < kMostSplits ? most : kMostSplits;
+  const int64_t need = ((int64_t)keys + kLeastKeys - 1) / kLeastKeys;
+  splits = (int)(need < most ? need : most);
+  if (splits < 1) splits = 1;
+  chunk = (int)(((int64_t)keys + splits - 1) / splits + 31) / 32 * 32;
+  if (chunk < kLeastKeys) chunk = kLeastKeys;
+}
+
+Plan plan_of(int B, int q_heads, int n_heads, int max_prefix, int max_rest) {
+  Plan p;
+  const int G = q_heads / n_heads, rows = B * G;
+  p.tile_rows = rows <= 16 ? 16 : rows <= 32 ? 32 : 64;
+  p.row_tiles = (rows + p.tile_rows - 1) / p.tile_rows;
+  p.head_tiles = (G + kRows - 1) / kRows;
+  divide(max_prefix, (int64_t)n_heads * p.row_tiles, p.splits, p.chunk);
+  divide(max_rest, (int64_t)n_heads * p.head_tiles * B, p.own_splits, p.own_chunk);
+  return p;
+}
+int64_t shared_rows(const Plan& p, int n_heads) {
+  return (int64_t)n_heads * p.row_tiles * p.splits * p.tile_rows;
+}
+int64_t own_rows(const Plan& p, int B, int q_heads, int n_heads) {
+  const int G = q_heads / n_heads;
+  return (int64_t)n_heads * p.head_tiles * B * p.own_splits * (G < kRows ? G : kRows);
+}
+
+template <typename T, int DP>
+hipError_t run_prefix_d(const PrefixArgs& a, int tile_rows, hipStream_t s) {
+  const int grid = a.shared_groups + a.own_groups;
+  if (tile_rows == 16)
+    attn_prefix_kernel<T, DP, 1, 1><<<grid, kThreads, 0, s>>>(a);
+  else if (tile_rows == 32)
+    attn_prefix_kernel<T, DP, 1, 2><<<grid, kThreads, 0, s>>>(a);
+  else  // (wider rows leave no registers for two column sets)
+    attn_prefix_kernel<T, DP, DP <= 128 ? 2 : 1, DP <= 128 ? 2 : 4><<<grid, kThreads, 0, s>>>(a);
+  const hipError_t err = hipGetLastError();
+  if (err != hipSuccess) return err;
+  const int64_t rows = (int64_t)a.B * a.Hq;
+  attn_prefix_join_kernel<T><<<(rows + kWaves - 1) / kWaves, kThreads, 0, s>>>(a, tile_rows);
+  return hipGetLastError();
+}
+
+template <typename T>
+hipError_t run_prefix(const PrefixArgs& a, int tile_rows, hipStream_t s) {
+  if (a.D <= 64) return run_prefix_d<T, 64>(a, tile_rows, s);
+  if (a.D <= 128) return run_prefix_d<T, 128>(a, tile_rows, s);
+  return run_prefix_d<T, 256>(a, tile_rows, s);
+}
+
+}  // namespace
+
+size_t attn_prefix_workspace(int B, int q_heads, int n_heads, int dim, int max_prefix,
+                             int max_rest) {
+  if (B == 0) return 0;
+  const Plan p = plan_of(B, q_heads, n_heads, max_prefix, max_rest);
+  return (size_t)(shared_rows(p, n_heads) + own_rows(p, B, q_heads, n_heads)) * (dim + 2) *
+         sizeof(float);
+}
+
+hipError_t launch_attn_prefix(const void* q, int64_t q_stride, int B, int q_heads,
+                              const d2moe_kv_cache* c, const int32_t* table, int max_pages,
+                              const int32_t* lengths, const int32_t* prefix_table,
+                              int prefix_pages, const int32_t* prefix_lens, int max_prefix,
+                              int max_rest, float scale, void* out, void* ws, hipStream_t s) {
+  if (B == 0) return hipSuccess;
+  const Plan p = plan_of(B, q_heads, c->n_heads, max_prefix, max_rest);
+  PrefixArgs a{};
+  a.q = q, a.k = c->k, a.v = c->v, a.q_stride = q_stride, a.page_stride = c->page_stride;
+  a.token_stride = c->token_stride, a.head_stride = c->head_stride;
+  a.table = table, a.lengths = lengths, a.prefix_table = prefix_table;
+  a.prefix_lens = prefix_lens, a.page = fast_div(c->page_size);
+  a.B = B, a.n_pages = c->n_pages, a.max_pages = max_pages, a.prefix_pages = prefix_pages;
+  a.Hq = q_heads, a.H = c->n_heads, a.G = q_heads / c->n_heads, a.D = c->head_dim;
+  a.scale_log2 = scale * kLog2e;
+  a.row_tiles = p.row_tiles, a.splits = p.splits, a.chunk = p.chunk;
+  a.head_tiles = p.head_tiles, a.own_splits = p.own_splits, a.own_chunk = p.own_chunk;
+  a.shared_groups = c->n_heads * p.row_tiles * p.splits;
+  a.own_groups = c->n_heads * p.head_tiles * B * p.own_splits;
+  const int64_t rows = shared_rows(p, c->n_heads), own = own_rows(p, B, q_heads, c->n_heads);
+  a.shared_o = (float*)ws, a.own_o = a.shared_o + rows * a.D;
+  a.shared_ml = a.own_o + own * a.D, a.own_ml = a.shared_ml + rows * 2;
+  a.out = out;
+  return c->dtype == D2MOE_BF16 ? run_prefix<uint16_t>(a, p.tile_rows, s)
+                                : run_prefix<float>(a, p.tile_rows, s);
+}
+
+}  // namespace d2moe

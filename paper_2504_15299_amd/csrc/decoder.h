@@ -1,6 +1,6 @@
 // Internal declarations of the decode operators around the MoE layer: the
 // host-side launchers of linear.hip, linear_pack.hip, kv_append.hip,
-// attn_decode.hip, block_norm.hip and sample.hip.
+// attn_decode.hip, attn_prefix.hip, block_norm.hip and sample.hip.
 #pragma once
 
 #include "internal.h"
@@ -55,6 +55,14 @@ hipError_t launch_attn_decode(const void* q, int64_t q_stride, int B, int q_head
                               const d2moe_kv_cache* c, const int32_t* table, int max_pages,
                               const int32_t* lengths, int max_len, int window, float scale,
                               void* out, void* ws, hipStream_t s);
+
+size_t attn_prefix_workspace(int B, int q_heads, int n_heads, int dim, int max_prefix,
+                             int max_rest);
+hipError_t launch_attn_prefix(const void* q, int64_t q_stride, int B, int q_heads,
+                              const d2moe_kv_cache* c, const int32_t* table, int max_pages,
+                              const int32_t* lengths, const int32_t* prefix_table,
+                              int prefix_pages, const int32_t* prefix_lens, int max_prefix,
+                              int max_rest, float scale, void* out, void* ws, hipStream_t s);
 
 hipError_t launch_block_norm(float* x, float x_scale, const void* y, d2moe_dtype yd, float y_scale,
                              const float* post_w, const void* gate, d2moe_dtype gd,

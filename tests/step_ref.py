@@ -117,3 +117,32 @@ def sample(l, u, t=1.0, k=0, p=1.0, m=0.0):
     if u > 0:
         room = min(room, np.abs(run - at).min() / run[-1])
     return int(order[i]), w[i] / run[-1], room
+
+
+# ---- attention behind a shared prefix ----------------------------------------------------
+
+def attn_prefix(q, k, v, table, lengths, prefix_table, prefix_lens, scale):
+    """(out, bound on the error before the result's own rounding): decoder_ref.attn over
+    the rows of pages that each sequence really has."""
+    page, room = k.shape[1], len(prefix_table) * k.shape[1]
+    width = max(len(prefix_table), table.shape[1])
+    out, err = np.zeros_like(q), np.zeros_like(q)
+    for b in range(len(q)):
+        n = max(int(lengths[b]), 0)
+        s = min(max(int(prefix_lens[b]), 0), n, room)
+        n = max(min(n, table.shape[1] * page), s)
+        if n == 0:
+            continue
+        # every token as a page of its own
+        j = np.arange(n)
+        own = np.full(width, -1, np.int64)
+        own[:table.shape[1]] = table[b]
+        pre = np.full(width, -1, np.int64)
+        pre[:len(prefix_table)] = prefix_table
+        p = np.where(j < s, pre[j // page], own[j // page])
+        ok = (p >= 0) & (p < len(k))
+        at = np.where(ok, p * page + j % page, -1)
+        flat = lambda t: t.reshape(-1, 1, *t.shape[2:])  # noqa: E731
+        o, e = attn(q[b:b + 1], flat(k), flat(v), at[None], [n], scale)
+        out[b], err[b] = o[0], e[0]
+    return out, err

@@ -1,5 +1,7 @@
-"""Refusals of the entry points for head norms with the append, on the host: nothing
-is launched (the pointers are fake and would fault if used)."""
+"""Refusals of the normed append, scored routing, sampling and shared-prefix attention,
+on the host: nothing is launched (the pointers are fake and would fault if used)."""
+import ctypes
+
 import pytest
 import torch
 
@@ -94,3 +96,38 @@ def test_sample_binding_refusals():
             api.sample(**{**dict(logits=x, u=u), **kw})
     with pytest.raises(TypeError):
         api.sample(x.half(), u)
+
+
+def test_attn_prefix_refusals():
+    ok = dict(q=FAKE, qs=512, B=3, h=8, c=cache(), bt=FAKE, mp=300, ln=FAKE, pt=FAKE, pp=200,
+              pl=FAKE, mx=3200, mr=1600, sc=0.125, o=FAKE, ws=FAKE, n=1 << 40, s=None)
+    refuses("d2moe_attn_prefix", ok, [dict(c=cache(**b)) for b in BAD_CACHES])
+    refuses("d2moe_attn_prefix", ok, [
+        dict(q=None), dict(o=None), dict(ln=None), dict(bt=None), dict(pt=None), dict(pl=None),
+        dict(q=ODD), dict(o=ODD), dict(qs=504), dict(qs=516), dict(B=-1), dict(B=65536),
+        dict(B=65535, h=128, qs=8192), dict(h=0), dict(h=6), dict(h=3), dict(h=65536),
+        dict(mp=-1), dict(mp=(1 << 26) + 1), dict(pp=-1), dict(pp=(1 << 26) + 1), dict(mx=-1),
+        dict(mr=-1), dict(mx=(1 << 30) + 1), dict(mr=(1 << 30) + 1), dict(sc=float("nan")),
+        dict(sc=float("inf")), dict(sc=2.5e38)])
+    refuses("d2moe_attn_prefix", ok, [dict(ws=None), dict(ws=ODD), dict(n=16)], api.EWORKSPACE)
+    refuses("d2moe_attn_prefix", ok, [dict(B=0)], api.OK)
+
+
+def test_attn_prefix_workspace():
+    """Grows with either length expected."""
+    n = ctypes.c_size_t()
+
+    def need(*a):
+        assert api.lib().d2moe_attn_prefix_workspace(*a, ctypes.byref(n)) == 0
+        return n.value
+
+    assert need(0, 8, 8, 64, 10 ** 6, 10 ** 6) == 0 < need(1, 1, 1, 8, 0, 0)
+    for B, hq, h, d in ((1, 8, 2, 64), (16, 32, 8, 128), (64, 32, 8, 128), (9, 12, 12, 256)):
+        last = 0
+        for length in list(range(0, 20000, 37)) + [1 << 30]:
+            assert need(B, hq, h, d, length, length // 3) >= last
+            last = need(B, hq, h, d, length, length // 3)
+    for args in ((-1, 8, 8, 64, 1, 1), (1, 7, 2, 64, 1, 1), (1, 8, 8, 60, 1, 1),
+                 (1, 8, 8, 64, -1, 1), (1, 8, 8, 64, 1, -1)):
+        assert api.lib().d2moe_attn_prefix_workspace(*args, ctypes.byref(n)) == api.EINVAL
+    assert api.lib().d2moe_attn_prefix_workspace(1, 8, 8, 64, 1, 1, None) == api.EINVAL
