@@ -110,7 +110,8 @@ def sample(l, u, t=1.0, k=0, p=1.0, m=0.0):
         room = min(room, np.abs(run - at).min() / run[-1]) if p > 0 else room
     if m > 0:
         n = min(n, int((w >= min(m, 1.0)).sum()))
-        room = min(room, np.abs(w[1:] - m).min()) if len(w) > 1 and m < 1 else room
+        # (w itself is compared with m, not its units: off by 2^-42 of itself)
+        room = min(room, np.abs(w[1:] / m - 1).min()) if len(w) > 1 and m < 1 else room
     run = np.cumsum(w[:n])
     at = min(max(u, 0.0), 1.0) * run[-1]
     i = min(int((run <= at).sum()), n - 1)

@@ -79,6 +79,18 @@ def test_temperatures(t, k, p):
     run(normal(16, 9001), rng.random(16), t, k, p)
 
 
+@pytest.mark.parametrize("dtype", [F32, BF])
+@pytest.mark.parametrize("k", [None, 3, 500, 512, 513, 2000])
+@pytest.mark.parametrize("p", [None, 0.2, 0.999])
+@pytest.mark.parametrize("m", [None, 0.9, 0.05, 1e-6])
+def test_bounds_of_flat_rows(m, p, k, dtype):
+    """Rows of which min-p or top-k leave a few tokens, some hundred or thousands, and in
+    which top-p ends before or after them; logits that fill one bin, or many."""
+    rng = np.random.default_rng(9)
+    for V, std in ((700, 0.5), (6001, 0.02), (6001, 1.0), (20000, 4.0)):
+        run(normal(6, V, dtype, std), rng.random(6), rng.uniform(0.5, 1.5, 6), k, p, m)
+
+
 def test_temperature_zero_takes_the_largest():
     x = normal(9, 5000)
     x[3, 77] = x[3, 4000] = 50.0
