@@ -19,14 +19,19 @@
 namespace d2moe {
 namespace {
 
-constexpr int kThreads = 256, kWaves = 4;
+constexpr int kThreads = 256, kWaves = 4, kTurn = 256;
 constexpr int kRows = 16;  // queries of a lane column set
+// How far (in units of log2) scores may lie above the reference that they are weighed
+// by: it is the largest score when it is set, and moves only past this, so that most
+// tiles neither look for the largest among lanes nor rescale the value sums.
+constexpr float kRoom = 8.0f;
+constexpr int kSpan = 512;  // keys whose row offsets are worked out at a time
 
 struct PrefixArgs {
   const void *q, *k, *v;
   int64_t q_stride, page_stride, token_stride, head_stride;
   const int32_t *table, *lengths, *prefix_table, *prefix_lens;
-  FastDiv page;
+  FastDiv page, per_head;  // (per_head: by G)
   int B, n_pages, max_pages, prefix_pages, Hq, H, G, D;
   float scale_log2;  // scale / ln 2
   int row_tiles, splits, chunk;           // of the prefix: row tiles, runs of `chunk` keys
@@ -127,17 +132,23 @@ struct Products<uint16_t, DP> {
           x[j][0] = w.x, x[j][1] = w.y;
         }
       }
+      // four elements at a time, so that no product waits for the one before it
 #pragma unroll
-      for (int i = 0; i < VE; ++i) {
-        u4 a;
+      for (int i0 = 0; i0 < VE; i0 += 4) {
+        u4 a[4];
 #pragma unroll
-        for (int d = 0; d < 4; ++d)
-          a[d] = __builtin_amdgcn_perm(x[2 * d + 1][i / 2], x[2 * d][i / 2],
-                                       (i & 1) ? 0x07060302u : 0x05040100u);
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+          for (int d = 0; d < 4; ++d)
+            a[i][d] = __builtin_amdgcn_perm(x[2 * d + 1][(i0 + i) / 2], x[2 * d][(i0 + i) / 2],
+                                            (i & 1) ? 0x07060302u : 0x05040100u);
 #pragma unroll
         for (int k = 0; k < 3; ++k)
 #pragma unroll
-          for (int ct = 0; ct < CT; ++ct) o[ct][h][i] = mma(a, p[ct].piece[k], o[ct][h][i]);
+          for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int ct = 0; ct < CT; ++ct)
+              o[ct][h][i0 + i] = mma(a[i], p[ct].piece[k], o[ct][h][i0 + i]);
       }
     }
   }
@@ -204,9 +215,10 @@ struct Run {
   static constexpr int NG = kWaves / NC, KEYS = NG * M::TK, ROWS = 16 * CT * NC;
   static constexpr int EACH = KEYS * M::CPR / kThreads;  // chunks of K, and of V, a thread
   static_assert(KEYS * M::CPR % kThreads == 0, "whole chunks");
+  static_assert(kSpan % KEYS == 0, "whole steps");
   struct Step {
+    int64_t off[2][kSpan];  // of the keys' rows, -1 where there is none: spans in turn
     u4 k[KEYS * M::CPR], v[KEYS * M::CPR];
-    float none[KEYS];  // 0, or -infinity where there is no key
   };
   struct Join {
     float m[NG][ROWS], l[NG][ROWS];
@@ -256,92 +268,139 @@ __device__ void attend(const PrefixArgs& a, typename Run<T, DP, CT, NC>::Lds& ld
       for (int i = 0; i < M::VE; ++i) o[ct][h][i] = f4{0.0f, 0.0f, 0.0f, 0.0f};
   }
 
-  // chunk e of this thread: row (e kThreads + tid) / CPR of the step, chunk tid % CPR
-  const int c = tid % CPR;
-  const bool wide = c * PER < a.D;
-  int page[EACH];
-  u4 kf[EACH], vf[EACH];
-  uint32_t have = 0;
-  auto fetch = [&](int s) {  // the pages of step s
+  // Row offsets by all threads, a span at a time: written to LDS where the span before
+  // it begins, their block-table entries read a span earlier.
+  constexpr int kOwn = kSpan / kThreads, kPer = kSpan / R::KEYS;
+  const int steps = (k1 - k0 + R::KEYS - 1) / R::KEYS, spans = (steps + kPer - 1) / kPer;
+  int page[kOwn];
+  auto fetch = [&](int span) {
 #pragma unroll
-    for (int e = 0; e < EACH; ++e) {
-      const uint32_t key = k0 + s * R::KEYS + (e * kThreads + tid) / CPR;
-      const uint32_t at = a.page.div(key);
+    for (int e = 0; e < kOwn; ++e) {
+      const uint32_t at = a.page.div(k0 + span * kSpan + e * kThreads + tid);
       page[e] = table[at < (uint32_t)pages ? at : (uint32_t)pages - 1];
     }
   };
-  auto load = [&](int s) {  // and their rows: whatever row where there is no key
-    have = 0;
+  auto put = [&](int span) {
 #pragma unroll
-    for (int e = 0; e < EACH; ++e) {
-      const uint32_t key = k0 + s * R::KEYS + (e * kThreads + tid) / CPR;
+    for (int e = 0; e < kOwn; ++e) {
+      const uint32_t key = k0 + span * kSpan + e * kThreads + tid;
       const bool in = key < (uint32_t)k1 && (uint32_t)page[e] < (uint32_t)a.n_pages;
-      const int64_t at = in ? page[e] * a.page_stride +
-                                  (int64_t)(key - a.page.div(key) * a.page.d) * a.token_stride
-                            : 0;
-      const int d = wide ? c * PER : 0;
-      kf[e] = *(const u4*)(kc + at + d);
-      vf[e] = *(const u4*)(vc + at + d);
-      have |= (in ? 1u : 0u) << e;
+      lds.step.off[span & 1][e * kThreads + tid] =
+          in ? page[e] * a.page_stride +
+                   (int64_t)(key - a.page.div(key) * a.page.d) * a.token_stride
+             : -1;
     }
   };
-  const int steps = (k1 - k0 + R::KEYS - 1) / R::KEYS;
+  // chunk e of this thread: row (e kThreads + tid) / CPR of the step, chunk tid % CPR;
+  // chunks past the head's end are zero
+  const int c = tid % CPR;
+  const bool wide = c * PER < a.D;
+  const T *kd = kc + c * PER, *vd = vc + c * PER;
+  u4 kf[EACH], vf[EACH];
+#pragma unroll
+  for (int e = 0; e < EACH; ++e) kf[e] = vf[e] = u4{0, 0, 0, 0};
+  uint32_t holes = 0;
+  auto load = [&](int s) {  // whatever row where there is no key
+    const int64_t* off = lds.step.off[s / kPer & 1] + s % kPer * R::KEYS;
+    holes = 0;
+    int64_t at[EACH];
+#pragma unroll
+    for (int e = 0; e < EACH; ++e) at[e] = off[(e * kThreads + tid) / CPR];
+#pragma unroll
+    for (int e = 0; e < EACH; ++e) {
+      holes |= (at[e] < 0 ? 1u : 0u) << e;
+      at[e] = at[e] < 0 ? 0 : at[e];
+    }
+    if (wide) {
+#pragma unroll
+      for (int e = 0; e < EACH; ++e) kf[e] = *(const u4*)(kd + at[e]);
+#pragma unroll
+      for (int e = 0; e < EACH; ++e) vf[e] = *(const u4*)(vd + at[e]);
+    }
+  };
   fetch(0);
+  put(0);
+  if (spans > 1) fetch(1);
+  lds_barrier();
   load(0);
-  if (steps > 1) fetch(1);
   for (int s = 0; s < steps; ++s) {
     lds_barrier();  // the step before has been used
+    if (__any(holes)) {  // 0 times what a masked row holds is not 0
+#pragma unroll
+      for (int e = 0; e < EACH; ++e)
+        if (holes >> e & 1) vf[e] = u4{0, 0, 0, 0};
+    }
 #pragma unroll
     for (int e = 0; e < EACH; ++e) {
       const int row = (e * kThreads + tid) / CPR;
-      const bool in = have >> e & 1, live = in && wide;
-      const u4 zero = {0, 0, 0, 0};  // not what a masked row holds: 0 times it is not 0
-      lds.step.k[row * CPR + (c ^ swizzle<CPR>(row))] = live ? kf[e] : zero;
-      lds.step.v[row * CPR + c] = live ? vf[e] : zero;
-      if (c == 0) lds.step.none[row] = in ? 0.0f : -INFINITY;
+      lds.step.k[row * CPR + (c ^ swizzle<CPR>(row))] = kf[e];
+      lds.step.v[row * CPR + c] = vf[e];
     }
+    const int span = s / kPer;
+    if (s % kPer == 0 && span + 1 < spans) put(span + 1);
     lds_barrier();
     if (s + 1 < steps) load(s + 1);
-    if (s + 2 < steps) fetch(s + 2);
+    if (s % kPer == 0 && span + 2 < spans) fetch(span + 2);
 
+    // the keys of this wave's tile that are none
+    const uint32_t none = (uint32_t)__ballot(
+        lds.step.off[span & 1][s % kPer * R::KEYS + kg * M::TK + (lane & (M::TK - 1))] < 0);
     f4 sc[CT][M::NS / 4];
     M::scores(sc, lds.step.k + kg * M::TK * CPR, qf, lane);
     const int first = k0 + s * R::KEYS + kg * M::TK;
     const bool border = __any(first + M::TK > least);
-    typename M::P p[CT];
+    // scores in units of log2, less the reference m; above kRoom the reference moves
+    float x[CT][M::NS], mx[CT];
+    bool moves = false;
 #pragma unroll
     for (int ct = 0; ct < CT; ++ct) {
-      float x[M::NS], mx = -INFINITY;
+      const float ref = m[ct] == -INFINITY ? 0.0f : m[ct];
 #pragma unroll
-      for (int t = 0; t < M::NS / 4; ++t) {
-        const f4 none = *(const f4*)&lds.step.none[kg * M::TK + 16 * t + 4 * q];
+      for (int j = 0; j < M::NS; ++j) x[ct][j] = fmaf(sc[ct][j / 4][j % 4], a.scale_log2, -ref);
+    }
+    if (none != 0 || border) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const int j = 4 * t + i;
-          x[j] = fmaf(sc[ct][t][i], a.scale_log2, none[i]);
-          if (border && first + M::key_of(j, q) >= limit[ct]) x[j] = -INFINITY;
-          mx = fmaxf(mx, x[j]);
+      for (int ct = 0; ct < CT; ++ct)
+#pragma unroll
+        for (int j = 0; j < M::NS; ++j) {
+          const int key = M::key_of(j, q);
+          if ((none >> key & 1) || first + key >= limit[ct]) x[ct][j] = -INFINITY;
         }
-      }
-      mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
-      mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
-      const float m_new = fmaxf(m[ct], mx);
-      const float ref = m_new == -INFINITY ? 0.0f : m_new;  // nothing but masked keys so far
-      const float alpha = fast_exp2(m[ct] - ref);
-      m[ct] = m_new;
-      l[ct] *= alpha;
+    }
 #pragma unroll
-      for (int j = 0; j < M::NS; ++j) {
-        x[j] = fast_exp2(x[j] - ref);
-        l[ct] += x[j];
-      }
-      if (__any(alpha != 1.0f)) {
+    for (int ct = 0; ct < CT; ++ct) {
+      mx[ct] = -INFINITY;
+#pragma unroll
+      for (int j = 0; j < M::NS; ++j) mx[ct] = fmaxf(mx[ct], x[ct][j]);
+      moves |= mx[ct] > (m[ct] == -INFINITY ? -INFINITY : kRoom);
+    }
+    if (__any(moves)) {
+#pragma unroll
+      for (int ct = 0; ct < CT; ++ct) {
+        mx[ct] = fmaxf(mx[ct], __shfl_xor(mx[ct], 16, 64));
+        mx[ct] = fmaxf(mx[ct], __shfl_xor(mx[ct], 32, 64));
+        // the largest score so far, where there is one
+        const float ref = m[ct] == -INFINITY ? 0.0f : m[ct], top = fmaxf(m[ct], ref + mx[ct]);
+        const float by = top == -INFINITY ? 0.0f : top - ref, alpha = fast_exp2(m[ct] - ref - by);
+        m[ct] = top;
+        l[ct] *= alpha;
+#pragma unroll
+        for (int j = 0; j < M::NS; ++j) x[ct][j] -= by;
 #pragma unroll
         for (int h = 0; h < M::H; ++h)
 #pragma unroll
           for (int i = 0; i < M::VE; ++i) o[ct][h][i] *= alpha;
       }
-      M::split(p[ct], x);
+    }
+    typename M::P p[CT];
+#pragma unroll
+    for (int ct = 0; ct < CT; ++ct) {
+#pragma unroll
+      for (int j = 0; j < M::NS; ++j) {
+        x[ct][j] = fast_exp2(x[ct][j]);
+        l[ct] += x[ct][j];
+      }
+      M::split(p[ct], x[ct]);
     }
     M::values(o, p, lds.step.v + kg * M::TK * CPR, lane);
   }
@@ -367,23 +426,29 @@ __device__ void attend(const PrefixArgs& a, typename Run<T, DP, CT, NC>::Lds& ld
               f4{o[ct][h][i][e], o[ct][h][i + 1][e], o[ct][h][i + 2][e], o[ct][h][i + 3][e]};
   }
   lds_barrier();
-  const int row4 = a.D / 4;
-  for (int i = tid; i < rows * row4; i += kThreads) {
-    const int r = i / row4, d = (i - r * row4) * 4;
+  if (tid < R::ROWS) {  // the groups' factors, in the place of m
     float mm = -INFINITY, ll = 0.0f;
-    f4 acc = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-    for (int g = 0; g < R::NG; ++g) mm = fmaxf(mm, lds.join.m[g][r]);
+    for (int g = 0; g < R::NG; ++g) mm = fmaxf(mm, lds.join.m[g][tid]);
     const float ref = mm == -INFINITY ? 0.0f : mm;
 #pragma unroll
     for (int g = 0; g < R::NG; ++g) {
-      const float f = fast_exp2(lds.join.m[g][r] - ref);
-      ll = fmaf(f, lds.join.l[g][r], ll);
-      acc += f * *(const f4*)&lds.join.o[g][r][d];
+      const float f = fast_exp2(lds.join.m[g][tid] - ref);
+      ll = fmaf(f, lds.join.l[g][tid], ll);
+      lds.join.m[g][tid] = f;
     }
-    *(f4*)(part_o + (int64_t)r * a.D + d) = acc;
-    if (d == 0) *(float2*)(part_ml + 2 * r) = make_float2(mm, ll);
+    if (tid < rows) *(float2*)(part_ml + 2 * tid) = make_float2(mm, ll);
   }
+  lds_barrier();
+  constexpr int kRow = DP / 4;  // threads of a row
+  const int d = tid % kRow * 4;
+  if (d < a.D)
+    for (int r = tid / kRow; r < rows; r += kThreads / kRow) {
+      f4 acc = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+      for (int g = 0; g < R::NG; ++g) acc += lds.join.m[g][r] * *(const f4*)&lds.join.o[g][r][d];
+      *(f4*)(part_o + (int64_t)r * a.D + d) = acc;
+    }
 }
 
 // Row tiles of the prefix, 16 CT NC rows each: query r of a key head is head r % G of
@@ -397,7 +462,7 @@ __device__ void attend_shared(const PrefixArgs& a, typename Run<T, DP, CT, NC>::
   __shared__ int last;
   if (threadIdx.x == 0) last = 0;
   __syncthreads();
-  if ((int)threadIdx.x < rows) atomicMax(&last, shared_end(a, (r0 + threadIdx.x) / a.G));
+  if ((int)threadIdx.x < rows) atomicMax(&last, shared_end(a, a.per_head.div(r0 + threadIdx.x)));
   __syncthreads();
   const int k0 = split * a.chunk;
   const int end = last, k1 = split + 1 < a.splits && k0 + a.chunk < end ? k0 + a.chunk : end;
@@ -406,10 +471,10 @@ __device__ void attend_shared(const PrefixArgs& a, typename Run<T, DP, CT, NC>::
       a, lds, a.prefix_table, a.prefix_pages, hk, k0, k1,
       [&](int r) -> const T* {
         if (r >= rows) return nullptr;
-        const int b = (r0 + r) / a.G, g = r0 + r - b * a.G;
+        const int b = a.per_head.div(r0 + r), g = r0 + r - b * a.G;
         return (const T*)a.q + b * a.q_stride + (int64_t)(hk * a.G + g) * a.D;
       },
-      [&](int r) { return r < rows ? shared_end(a, (r0 + r) / a.G) : 0x7fffffff; }, rows,
+      [&](int r) { return r < rows ? shared_end(a, a.per_head.div(r0 + r)) : 0x7fffffff; }, rows,
       a.shared_o + part * a.D, a.shared_ml + part * 2);
 }
 
@@ -433,7 +498,7 @@ __device__ void attend_own(const PrefixArgs& a, typename Run<T, DP, 1, 1>::Lds& 
       [&](int) { return 0x7fffffff; }, rows, a.own_o + part * a.D, a.own_ml + part * 2);
 }
 
-// Both kinds of workgroups in turns of eight (one on each die).
+// Both kinds of workgroups in turns of kTurn, one a CU.
 template <typename T, int DP, int CT, int NC>
 __global__ __launch_bounds__(kThreads, DP <= 128 ? 2 : 1) void attn_prefix_kernel(PrefixArgs a) {
   union Lds {
@@ -443,9 +508,9 @@ __global__ __launch_bounds__(kThreads, DP <= 128 ? 2 : 1) void attn_prefix_kerne
   __shared__ Lds lds;
   const int i = blockIdx.x;
   const int both =
-      (a.shared_groups < a.own_groups ? a.shared_groups : a.own_groups) / 8 * 8;
-  int u = i / 16 * 8 + i % 8;
-  bool shared = i % 16 < 8;
+      (a.shared_groups < a.own_groups ? a.shared_groups : a.own_groups) / kTurn * kTurn;
+  int u = i / (2 * kTurn) * kTurn + i % kTurn;
+  bool shared = i % (2 * kTurn) < kTurn;
   if (i >= 2 * both) {
     u = i - both;
     shared = u < a.shared_groups;
@@ -457,60 +522,85 @@ __global__ __launch_bounds__(kThreads, DP <= 128 ? 2 : 1) void attn_prefix_kerne
     attend_own<T, DP>(a, lds.own, u);
 }
 
-// Joins the parts of a query, one wave each: the prefix's runs, then its own.  Half waves
-// take parts in turn where a row has no more than 128 values.
-template <typename T>
+// Joins the parts of a query, a workgroup each: the prefix's runs, then its own, one
+// after the other by parts of a wave (half a wave has 128 values), four of them loaded
+// together.
+template <typename T, int LANES>
 __global__ __launch_bounds__(kThreads) void attn_prefix_join_kernel(PrefixArgs a, int tile_rows) {
-  const int64_t row = (int64_t)blockIdx.x * kWaves + (threadIdx.x >> 6);
-  if (row >= (int64_t)a.B * a.Hq) return;
-  const int b = (int)(row / a.Hq), head = (int)(row - (int64_t)b * a.Hq);
-  const int hk = head / a.G, g = head - hk * a.G, lane = threadIdx.x & 63;
-  const int wide = a.D <= 128 ? 32 : 64, lanes = 64 / wide, sub = lane / wide;
-  const int d = 4 * (lane % wide), own_rows = a.G < kRows ? a.G : kRows;
+  constexpr int kSubs = kThreads / LANES, kAhead = 4;
+  __shared__ float pm[kSubs], pl[kSubs];
+  __shared__ __align__(16) f4 po[kSubs][LANES];
+  const int head = blockIdx.x, b = blockIdx.y;
+  const int hk = head / a.G, g = head - hk * a.G;
+  const int sub = threadIdx.x / LANES, lane = threadIdx.x % LANES, d = 4 * lane < a.D ? 4 * lane : 0;
+  const int own_rows = a.G < kRows ? a.G : kRows;
   const int r = b * a.G + g, tile = r / tile_rows, n = a.splits + a.own_splits;
   float mm = -INFINITY, ll = 0.0f;
   f4 acc = {0.0f, 0.0f, 0.0f, 0.0f};
-  for (int i = sub; i < n; i += lanes) {
-    const float *po, *pm;
-    if (i < a.splits) {
-      const int64_t p = (((int64_t)i * a.row_tiles + tile) * a.H + hk) * tile_rows + r % tile_rows;
-      po = a.shared_o + p * a.D, pm = a.shared_ml + p * 2;
-    } else {
-      const int64_t u = (((int64_t)(i - a.splits) * a.B + b) * a.head_tiles + g / kRows) * a.H + hk;
-      const int64_t p = u * own_rows + g % kRows;
-      po = a.own_o + p * a.D, pm = a.own_ml + p * 2;
-    }
-    const float2 ml = *(const float2*)pm;
-    if (ml.x == -INFINITY) continue;  // no key of it, and maybe no values written
-    const f4 v = d < a.D ? *(const f4*)(po + d) : f4{0.0f, 0.0f, 0.0f, 0.0f};
-    const float top = fmaxf(mm, ml.x), was = fast_exp2(mm - top), f = fast_exp2(ml.x - top);
-    mm = top;
-    ll = fmaf(f, ml.y, ll * was);
-    acc = acc * was + f * v;
-  }
-  if (lanes == 2) {
-    const float other = __shfl_xor(mm, 32, 64), top = fmaxf(mm, other);
-    const float f = fast_exp2(mm - (top == -INFINITY ? 0.0f : top));
-    ll *= f;
-    acc *= f;
-    ll += __shfl_xor(ll, 32, 64);
+  for (int i0 = sub; i0 < n; i0 += kAhead * kSubs) {
+    float2 ml[kAhead];
+    f4 v[kAhead];
 #pragma unroll
-    for (int e = 0; e < 4; ++e) acc[e] += __shfl_xor(acc[e], 32, 64);
+    for (int e = 0; e < kAhead; ++e) {
+      const int i = i0 + e * kSubs < n ? i0 + e * kSubs : i0;
+      const float *o, *m;
+      if (i < a.splits) {
+        const int64_t p =
+            (((int64_t)i * a.row_tiles + tile) * a.H + hk) * tile_rows + r % tile_rows;
+        o = a.shared_o + p * a.D, m = a.shared_ml + p * 2;
+      } else {
+        const int64_t u = (((int64_t)(i - a.splits) * a.B + b) * a.head_tiles + g / kRows) * a.H + hk;
+        const int64_t p = u * own_rows + g % kRows;
+        o = a.own_o + p * a.D, m = a.own_ml + p * 2;
+      }
+      ml[e] = *(const float2*)m;
+      v[e] = *(const f4*)(o + d);
+    }
+    float top = mm;
+#pragma unroll
+    for (int e = 0; e < kAhead; ++e) top = fmaxf(top, ml[e].x);
+    const float was = fast_exp2(mm - (top == -INFINITY ? 0.0f : top));
+    mm = top;
+    ll *= was;
+    acc *= was;
+#pragma unroll
+    for (int e = 0; e < kAhead; ++e) {
+      // without a key there may be no values written
+      if (i0 + e * kSubs >= n || ml[e].x == -INFINITY) continue;
+      const float f = fast_exp2(ml[e].x - mm);
+      ll = fmaf(f, ml[e].y, ll);
+      acc += f * v[e];
+    }
   }
-  if (sub == 0 && d < a.D)
-    store4((T*)a.out + row * a.D + d, acc * (ll == 0.0f ? 0.0f : 1.0f / ll));
+  po[sub][lane] = acc;
+  if (lane == 0) pm[sub] = mm, pl[sub] = ll;
+  __syncthreads();
+  if (sub != 0 || 4 * lane >= a.D) return;
+#pragma unroll
+  for (int i = 1; i < kSubs; ++i) mm = fmaxf(mm, pm[i]);
+  const float ref = mm == -INFINITY ? 0.0f : mm;
+  ll = 0.0f;
+  acc = f4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+  for (int i = 0; i < kSubs; ++i) {
+    const float f = fast_exp2(pm[i] - ref);
+    ll = fmaf(f, pl[i], ll);
+    acc += f * po[i][lane];
+  }
+  store4((T*)a.out + ((int64_t)b * a.Hq + head) * a.D + d,
+         acc * (ll == 0.0f ? 0.0f : 1.0f / ll));
 }
 
 // How a call is divided, from the sizes alone.
 struct Plan {
   int tile_rows, row_tiles, splits, chunk, head_tiles, own_splits, own_chunk;
 };
-constexpr int kGroups = 512;     // of each kind, two a CU
+constexpr int kSharedGroups = 256, kOwnGroups = 512;
 constexpr int kLeastKeys = 128;  // of a run
 constexpr int kMostSplits = 64;
 
-void divide(int keys, int64_t units, int& splits, int& chunk) {
-  int64_t most = units >= kGroups ? 1 : kGroups / units;
+void divide(int keys, int64_t units, int groups, int& splits, int& chunk) {
+  int64_t most = units >= groups ? 1 : groups / units;
   most = most < kMostSplits ? most : kMostSplits;
   const int64_t need = ((int64_t)keys + kLeastKeys - 1) / kLeastKeys;
   splits = (int)(need < most ? need : most);
@@ -525,8 +615,8 @@ Plan plan_of(int B, int q_heads, int n_heads, int max_prefix, int max_rest) {
   p.tile_rows = rows <= 16 ? 16 : rows <= 32 ? 32 : 64;
   p.row_tiles = (rows + p.tile_rows - 1) / p.tile_rows;
   p.head_tiles = (G + kRows - 1) / kRows;
-  divide(max_prefix, (int64_t)n_heads * p.row_tiles, p.splits, p.chunk);
-  divide(max_rest, (int64_t)n_heads * p.head_tiles * B, p.own_splits, p.own_chunk);
+  divide(max_prefix, (int64_t)n_heads * p.row_tiles, kSharedGroups, p.splits, p.chunk);
+  divide(max_rest, (int64_t)n_heads * p.head_tiles * B, kOwnGroups, p.own_splits, p.own_chunk);
   return p;
 }
 int64_t shared_rows(const Plan& p, int n_heads) {
@@ -548,8 +638,8 @@ hipError_t run_prefix_d(const PrefixArgs& a, int tile_rows, hipStream_t s) {
     attn_prefix_kernel<T, DP, DP <= 128 ? 2 : 1, DP <= 128 ? 2 : 4><<<grid, kThreads, 0, s>>>(a);
   const hipError_t err = hipGetLastError();
   if (err != hipSuccess) return err;
-  const int64_t rows = (int64_t)a.B * a.Hq;
-  attn_prefix_join_kernel<T><<<(rows + kWaves - 1) / kWaves, kThreads, 0, s>>>(a, tile_rows);
+  attn_prefix_join_kernel<T, DP <= 128 ? 32 : 64>
+      <<<dim3(a.Hq, a.B), kThreads, 0, s>>>(a, tile_rows);
   return hipGetLastError();
 }
 
@@ -582,6 +672,7 @@ hipError_t launch_attn_prefix(const void* q, int64_t q_stride, int B, int q_head
   a.token_stride = c->token_stride, a.head_stride = c->head_stride;
   a.table = table, a.lengths = lengths, a.prefix_table = prefix_table;
   a.prefix_lens = prefix_lens, a.page = fast_div(c->page_size);
+  a.per_head = fast_div(q_heads / c->n_heads);
   a.B = B, a.n_pages = c->n_pages, a.max_pages = max_pages, a.prefix_pages = prefix_pages;
   a.Hq = q_heads, a.H = c->n_heads, a.G = q_heads / c->n_heads, a.D = c->head_dim;
   a.scale_log2 = scale * kLog2e;
