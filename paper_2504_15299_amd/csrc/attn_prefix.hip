@@ -31,7 +31,7 @@ struct PrefixArgs {
   const void *q, *k, *v;
   int64_t q_stride, page_stride, token_stride, head_stride;
   const int32_t *table, *lengths, *prefix_table, *prefix_lens;
-  FastDiv page, per_head;  // (per_head: by G)
+  FastDiv page, per_head, by_heads, by_tiles, by_head_tiles, by_seqs;  // (per_head: by G)
   int B, n_pages, max_pages, prefix_pages, Hq, H, G, D;
   float scale_log2;  // scale / ln 2
   int row_tiles, splits, chunk;           // of the prefix: row tiles, runs of `chunk` keys
@@ -267,7 +267,6 @@ __device__ void attend(const PrefixArgs& a, typename Run<T, DP, CT, NC>::Lds& ld
 #pragma unroll
       for (int i = 0; i < M::VE; ++i) o[ct][h][i] = f4{0.0f, 0.0f, 0.0f, 0.0f};
   }
-
   // Row offsets by all threads, a span at a time: written to LDS where the span before
   // it begins, their block-table entries read a span earlier.
   constexpr int kOwn = kSpan / kThreads, kPer = kSpan / R::KEYS;
@@ -456,14 +455,21 @@ __device__ void attend(const PrefixArgs& a, typename Run<T, DP, CT, NC>::Lds& ld
 template <typename T, int DP, int CT, int NC>
 __device__ void attend_shared(const PrefixArgs& a, typename Run<T, DP, CT, NC>::Lds& lds, int u) {
   constexpr int ROWS = Run<T, DP, CT, NC>::ROWS;
-  const int hk = u % a.H, tile = u / a.H % a.row_tiles, split = u / a.H / a.row_tiles;
+  const int v = a.by_heads.div(u), hk = u - v * a.H;
+  const int split = a.by_tiles.div(v), tile = v - split * a.row_tiles;
   const int r0 = tile * ROWS, total = a.B * a.G, rows = total - r0 < ROWS ? total - r0 : ROWS;
   // the end of the keys that any row attends
   __shared__ int last;
-  if (threadIdx.x == 0) last = 0;
-  __syncthreads();
-  if ((int)threadIdx.x < rows) atomicMax(&last, shared_end(a, a.per_head.div(r0 + threadIdx.x)));
-  __syncthreads();
+  if (threadIdx.x < 64) {  // (ROWS <= 64)
+    int n = (int)threadIdx.x < rows ? shared_end(a, a.per_head.div(r0 + threadIdx.x)) : 0;
+#pragma unroll
+    for (int off = 1; off < 64; off *= 2) {
+      const int other = __shfl_xor(n, off, 64);
+      n = other > n ? other : n;
+    }
+    if (threadIdx.x == 0) last = n;
+  }
+  lds_barrier();
   const int k0 = split * a.chunk;
   const int end = last, k1 = split + 1 < a.splits && k0 + a.chunk < end ? k0 + a.chunk : end;
   const int64_t part = (int64_t)u * ROWS;
@@ -481,8 +487,9 @@ __device__ void attend_shared(const PrefixArgs& a, typename Run<T, DP, CT, NC>::
 // A sequence's own tokens, 16 query heads of a key head at a time.
 template <typename T, int DP>
 __device__ void attend_own(const PrefixArgs& a, typename Run<T, DP, 1, 1>::Lds& lds, int u) {
-  const int hk = u % a.H, tile = u / a.H % a.head_tiles;
-  const int b = u / a.H / a.head_tiles % a.B, split = u / a.H / a.head_tiles / a.B;
+  const int v = a.by_heads.div(u), hk = u - v * a.H;
+  const int w = a.by_head_tiles.div(v), tile = v - w * a.head_tiles;
+  const int split = a.by_seqs.div(w), b = w - split * a.B;
   const int g0 = tile * kRows, rows = a.G - g0 < kRows ? a.G - g0 : kRows;
   const int from = shared_end(a, b), end = own_end(a, b);
   const int64_t k0 = from + (int64_t)split * a.own_chunk;
@@ -672,9 +679,11 @@ hipError_t launch_attn_prefix(const void* q, int64_t q_stride, int B, int q_head
   a.token_stride = c->token_stride, a.head_stride = c->head_stride;
   a.table = table, a.lengths = lengths, a.prefix_table = prefix_table;
   a.prefix_lens = prefix_lens, a.page = fast_div(c->page_size);
-  a.per_head = fast_div(q_heads / c->n_heads);
+  a.per_head = fast_div(q_heads / c->n_heads), a.by_heads = fast_div(c->n_heads);
   a.B = B, a.n_pages = c->n_pages, a.max_pages = max_pages, a.prefix_pages = prefix_pages;
   a.Hq = q_heads, a.H = c->n_heads, a.G = q_heads / c->n_heads, a.D = c->head_dim;
+  a.by_tiles = fast_div(p.row_tiles), a.by_head_tiles = fast_div(p.head_tiles);
+  a.by_seqs = fast_div(B);
   a.scale_log2 = scale * kLog2e;
   a.row_tiles = p.row_tiles, a.splits = p.splits, a.chunk = p.chunk;
   a.head_tiles = p.head_tiles, a.own_splits = p.own_splits, a.own_chunk = p.own_chunk;
