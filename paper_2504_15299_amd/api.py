@@ -10,7 +10,7 @@ from __future__ import annotations
 
 import ctypes
 import os
-from dataclasses import dataclass, replace
+from dataclasses import dataclass
 
 import torch
 
@@ -121,9 +121,11 @@ def lib():
         L.d2moe_block_norm.argtypes = [_P, f32, _P, _I, f32, _P, _P, _I, i64, _P, _I, _I, f32, _P,
                                        _I, _P]
         L.d2moe_sample.argtypes = [_P, _I, i64, _I, _I, _P, _P, _P, _P, _P, _P, _P, _P]
-        for name in ("d2moe_sample", "d2moe_attn_prefix_workspace", "d2moe_attn_prefix", "d2moe_linear_size", "d2moe_linear_pack", "d2moe_linear_pack_codes",
-                     "d2moe_linear_forward", "d2moe_kv_append", "d2moe_kv_append_norm", "d2moe_attn_decode_workspace",
-                     "d2moe_attn_decode", "d2moe_block_norm",
+        for name in ("d2moe_linear_size", "d2moe_linear_pack", "d2moe_linear_pack_codes",
+                     "d2moe_linear_forward", "d2moe_kv_append", "d2moe_kv_append_norm",
+                     "d2moe_attn_decode_workspace", "d2moe_attn_decode",
+                     "d2moe_attn_prefix_workspace", "d2moe_attn_prefix", "d2moe_block_norm",
+                     "d2moe_sample",
                      "d2moe_mwq_size", "d2moe_pack_mwq", "d2moe_debug_unpack", "d2moe_route",
                      "d2moe_mwq_calib_factor_workspace", "d2moe_mwq_calib_factor",
                      "d2moe_pack_mwq_calibrated_workspace", "d2moe_pack_mwq_calibrated",
@@ -342,7 +344,6 @@ def route_learned(x: torch.Tensor, Wg: torch.Tensor, bias, k: int, Wr: torch.Ten
 
 
 _SCORING = {"softmax": 0, "sigmoid": 1}
-_ROUTING_FIELDS = [f for f, _ in _Routing._fields_]
 
 
 def route_scored(logits, k: int, token_req, bit_table: torch.Tensor, scoring: str = "softmax",
@@ -373,30 +374,34 @@ def route_scored(logits, k: int, token_req, bit_table: torch.Tensor, scoring: st
         px, code = _arg(x, (T, d), x.dtype, dev, "x"), _CODES[x.dtype]
         pw = _arg(Wg, (E, d), f32, dev, "Wg")
         pb = None if bias is None else _arg(bias, (E,), f32, dev, "bias")
-    R, L = bit_table.shape[0], b_max - b_min + 1
+    R, L, slots = bit_table.shape[0], b_max - b_min + 1, T * k
     i32, u8 = torch.int32, torch.uint8
-    shapes = [((T, E), f32), ((T, k), i32), ((T, k), f32), ((T, k), u8), ((E, L), i32),
-              ((E * L + 1,), i32), ((T * k,), i32), ((T * k,), i32), ((E,), u8), ((1,), i32)]
-    given = range(len(shapes)) if logits is None else range(1, len(shapes))
     if out is None:
         if b_min > b_max or k < 1:
             raise ValueError("b_min <= b_max and k >= 1 are needed")
-        made = [logits] + [None] * 9
-        for i in given:
-            made[i] = _new(bit_table, *shapes[i], stream)
-        out = Routing(*made)
-    ptrs = [None if i not in given else
-            _arg(getattr(out, f), *shapes[i], dev, f) for i, f in enumerate(_ROUTING_FIELDS)]
-    if logits is not None:
-        ptrs[0] = pl
-        if out.logits is not logits:
-            out = replace(out, logits=logits)
+        shapes = [((T, k), i32), ((T, k), f32), ((T, k), u8), ((E, L), i32),
+                  ((E * L + 1,), i32), ((slots,), i32), ((slots,), i32), ((E,), u8), ((1,), i32)]
+        out = Routing(_new(bit_table, (T, E), f32, stream) if logits is None else logits,
+                      *[_new(bit_table, s, t, stream) for s, t in shapes])
+    if logits is None:
+        pl = _arg(out.logits, (T, E), f32, dev, "logits")
+    elif out.logits is not logits:
+        out = Routing(logits, out.topk_idx, out.topk_w, out.topk_bits, out.hist, out.offsets, out.perm,
+                      out.slot_of, out.expert_maxbit, out.flags)
+    c = _Routing(pl, _arg(out.topk_idx, (T, k), i32, dev, "topk_idx"),
+                 _arg(out.topk_w, (T, k), f32, dev, "topk_w"),
+                 _arg(out.topk_bits, (T, k), u8, dev, "topk_bits"),
+                 _arg(out.hist, (E, L), i32, dev, "hist"),
+                 _arg(out.offsets, (E * L + 1,), i32, dev, "offsets"),
+                 _arg(out.perm, (slots,), i32, dev, "perm"),
+                 _arg(out.slot_of, (slots,), i32, dev, "slot_of"),
+                 _arg(out.expert_maxbit, (E,), u8, dev, "expert_maxbit"),
+                 _arg(out.flags, (1,), i32, dev, "flags"))
     _run("d2moe_route_scored", dev, stream, px, code, T, d, pw, pb, E, k, _SCORING[scoring],
          None if select_bias is None else _arg(select_bias, (E,), f32, dev, "select_bias"), groups,
          top_groups, int(renorm), scale,
          None if token_req is None else _arg(token_req, (T,), i32, dev, "token_req"),
-         _arg(bit_table, (R, E), u8, dev, "bit_table"), R, b_min, b_max,
-         ctypes.byref(_Routing(*ptrs)))
+         _arg(bit_table, (R, E), u8, dev, "bit_table"), R, b_min, b_max, ctypes.byref(c))
     return out
 
 
@@ -502,8 +507,8 @@ def _new(like, shape, dtype, stream):
     the current stream has freed may still be in use there, so it is taken from
     ``stream``'s own, and kept until the current one is past its uses."""
     if stream is None:
-        if like.shape == shape and like.dtype == dtype and like.is_contiguous():
-            return torch.empty_like(like)  # the same, sooner
+        if like.shape == shape:  # the same, sooner
+            return torch.empty_like(like, dtype=dtype, memory_format=torch.contiguous_format)
         return like.new_empty(shape, dtype=dtype)
     with torch.cuda.stream(stream):
         t = like.new_empty(shape, dtype=dtype)
