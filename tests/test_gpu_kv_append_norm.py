@@ -98,6 +98,14 @@ def test_many_tokens(N, seqs, D, rot, dtype):
     run(N=N, seqs=seqs, H=1, Hq=2, D=D, rot=rot, x_dtype=dtype, dtype=dtype, page=32)
 
 
+# waves that keep some heads of 3 to 17 waves' worth over several tokens
+@pytest.mark.parametrize("N,H,Hq,D,rot", [(5001, 3, 11, 128, 128), (1700, 3, 11, 80, 20),
+                                          (9001, 2, 5, 64, 32)])
+@pytest.mark.parametrize("dtype", [BF, F32])
+def test_waves_that_stay(N, H, Hq, D, rot, dtype):
+    run(N=N, seqs=4, H=H, Hq=Hq, D=D, rot=rot, x_dtype=dtype, dtype=dtype, page=32)
+
+
 @pytest.mark.parametrize("dtype", [BF, F32])
 @pytest.mark.parametrize("D,rot,interleaved", [(64, 64, False), (64, 32, False), (80, 20, True),
                                                (256, 128, False), (256, 4, False)])
