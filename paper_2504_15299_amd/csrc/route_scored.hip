@@ -4,13 +4,16 @@
 //
 // Scores and their comparisons are binary64, so that the choice is that of the
 // formula wherever two scores differ by more than its last bits (binary32 would turn
-// one of 40000 choices among 64 experts); of a few hundred tokens a CU that is hidden
-// under the launches.
+// one of 40000 choices among 64 experts).  The comparisons are of integers in the same
+// order, the upper words first (as binary64, 8192 tokens' choices take 11.6 us for 9.3).
 //
-// Up to kOneTokens tokens everything is one workgroup.  Above, a wave a token
-// chooses, then every kBlock slots are counted, each key's counts scanned over the
+// Up to kOneTokens tokens everything is one workgroup (16 tokens, 2 of 8 experts: 6.0
+// us, latency: a load, the scores, the k maxima and seven barriers).  Above, a wave a
+// token chooses, then every kBlock slots are counted, each key's counts scanned over the
 // blocks, and the slots placed; the tables between the launches lie in the part of
-// slot_of that their block writes last.
+// slot_of that their block writes last.  8192 tokens, 6 of 64 experts in 4 of 8 groups,
+// sigmoid: 9.3 + 2.8 + 3.1 + 5.1 us, the choice bound by its instructions (3 MB cross
+// the memory, 0.6 us), the others by latency.
 #include "internal.h"
 
 namespace d2moe {
@@ -37,12 +40,20 @@ struct ScoredArgs {
 };
 
 template <int CTRL>
-__device__ inline double row_shift(double v) {  // lanes without a source keep their own
-  const uint64_t u = __builtin_bit_cast(uint64_t, v);
-  const int lo = (int)(uint32_t)u, hi = (int)(uint32_t)(u >> 32);
-  const uint32_t a = __builtin_amdgcn_update_dpp(lo, lo, CTRL, 0xf, 0xf, false);
-  const uint32_t b = __builtin_amdgcn_update_dpp(hi, hi, CTRL, 0xf, 0xf, false);
-  return __builtin_bit_cast(double, (uint64_t)b << 32 | a);
+__device__ inline int row_shift(int v) {  // lanes without a source keep their own
+  return __builtin_amdgcn_update_dpp(v, v, CTRL, 0xf, 0xf, false);
+}
+__device__ inline uint32_t larger(uint32_t a, uint32_t b) { return a > b ? a : b; }
+// The largest over the wave, on every lane: within rows of 16 by shifts, then over the
+// rows.
+__device__ inline uint32_t wave_max(uint32_t v) {
+  v = larger(v, row_shift<0x111>(v));
+  v = larger(v, row_shift<0x112>(v));
+  v = larger(v, row_shift<0x114>(v));
+  v = larger(v, row_shift<0x118>(v));
+  const uint32_t a = __builtin_amdgcn_readlane(v, 15), b = __builtin_amdgcn_readlane(v, 31);
+  const uint32_t c = __builtin_amdgcn_readlane(v, 47), d = __builtin_amdgcn_readlane(v, 63);
+  return larger(larger(a, b), larger(c, d));
 }
 __device__ inline double lane_value(double v, int lane) {  // lane uniform
   const uint64_t u = __builtin_bit_cast(uint64_t, v);
@@ -50,15 +61,14 @@ __device__ inline double lane_value(double v, int lane) {  // lane uniform
   const uint32_t b = __builtin_amdgcn_readlane((int)(uint32_t)(u >> 32), lane);
   return __builtin_bit_cast(double, (uint64_t)b << 32 | a);
 }
-// The largest over the wave, no NaN among them, on every lane: within rows of 16
-// by shifts, then over the rows.
-__device__ inline double wave_max(double v) {
-  v = fmax(v, row_shift<0x111>(v));
-  v = fmax(v, row_shift<0x112>(v));
-  v = fmax(v, row_shift<0x114>(v));
-  v = fmax(v, row_shift<0x118>(v));
-  return fmax(fmax(lane_value(v, 15), lane_value(v, 31)),
-              fmax(lane_value(v, 47), lane_value(v, 63)));
+// Integers in the order of the values, neither NaN nor -0.
+__device__ inline uint32_t ordered(float v) {
+  const uint32_t u = __builtin_bit_cast(uint32_t, v);
+  return u >> 31 ? ~u : u | 1u << 31;
+}
+__device__ inline uint64_t ordered(double v) {
+  const uint64_t u = __builtin_bit_cast(uint64_t, v);
+  return u >> 63 ? ~u : u | 1ull << 63;
 }
 __device__ inline double wave_sum(double v) {
   for (int off = 1; off < 64; off *= 2) v += __shfl_xor(v, off, 64);
@@ -76,7 +86,8 @@ __device__ inline void wave_handoff() {
 // the flag bits.  lkeys: where the slots' keys go as well.
 __device__ int select(const ScoredArgs& a, int t, int lane, double (&tmp)[64], int* lkeys) {
   const bool have = lane < a.E;
-  const double x = have ? (double)a.logits[(int64_t)t * a.E + lane] : -INFINITY;
+  const float logit = have ? a.logits[(int64_t)t * a.E + lane] : -INFINITY;
+  const double x = logit;
   int flag = 0, r = a.token_req ? a.token_req[t] : 0;
   if (r < 0 || r >= a.R) {
     flag = 2;
@@ -87,13 +98,14 @@ __device__ int select(const ScoredArgs& a, int t, int lane, double (&tmp)[64], i
   if (a.sigmoid) {
     score = 1.0 / (1.0 + exp(-x));
   } else {
-    const double top = wave_max(x == x ? x : -INFINITY);
+    const uint32_t most = wave_max(ordered(x == x ? logit + 0.0f : -INFINITY));
+    const double top = __builtin_bit_cast(float, most >> 31 ? most & ~(1u << 31) : ~most);
     const double e = !have || top == -INFINITY ? 0.0 : x == top ? 1.0 : exp(x - top);
     const double sum = wave_sum(e == e ? e : 0.0);
     score = sum == 0.0 ? 0.0 : e / sum;  // nothing but masked logits: no weight at all
   }
   const double by = have && a.select_bias ? score + (double)a.select_bias[lane] : score;
-  uint64_t avail = a.E >= 64 ? ~0ull : (1ull << a.E) - 1;
+  bool live = have;
   if (a.groups > 1) {
     // lane g sums the two best of group g, then counts the groups before it; NaN is
     // below everything
@@ -102,6 +114,7 @@ __device__ int select(const ScoredArgs& a, int t, int lane, double (&tmp)[64], i
     wave_handoff();
     double best = -INFINITY, next = -INFINITY;
     if (lane < a.groups)
+#pragma unroll 4
       for (int i = 0; i < size; ++i) {
         const double v = tmp[lane * size + i];
         next = fmax(next, fmin(best, v));
@@ -114,23 +127,29 @@ __device__ int select(const ScoredArgs& a, int t, int lane, double (&tmp)[64], i
     wave_handoff();
     int before = 0;
     if (lane < a.groups)
+#pragma unroll 4
       for (int g = 0; g < a.groups; ++g) before += tmp[g] > best || (tmp[g] == best && g < lane);
     wave_handoff();  // the next token's group values come after
     const uint64_t on = __ballot(lane < a.groups && before < a.top_groups);
-    avail = __ballot(have && (on >> (lane / size) & 1));
+    live = have && (on >> (lane / size) & 1);
   }
   double mine = 0.0, total = 0.0;
   int idx = 0, bits = 0;
-  const bool real = by == by;
+  // The largest by its upper word, by the lower one where several share that; NaN
+  // comes after -infinity, what may not be chosen after that.
+  const uint64_t key = by == by ? ordered(by + 0.0) : 1ull << 32;
+  uint32_t upper = live ? (uint32_t)(key >> 32) : 0;
   for (int i = 0; i < a.k; ++i) {
-    const bool live = avail >> lane & 1;
-    const double top = wave_max(live && real ? by : -INFINITY);
-    uint64_t cand = __ballot(live && by == top);
-    if (cand == 0) cand = avail;  // only NaN left
+    const uint32_t top = wave_max(upper);
+    uint64_t cand = __ballot(upper == top);
+    if (cand & (cand - 1)) {
+      const uint32_t low = upper == top ? (uint32_t)key : 0;
+      cand &= __ballot(low == wave_max(low));
+    }
     const int best = __builtin_amdgcn_readfirstlane(__ffsll((unsigned long long)cand) - 1);
     const double s = lane_value(score, best);
     const int bb = __builtin_amdgcn_readlane(b, best);
-    avail &= ~(1ull << best);
+    if (lane == best) upper = 0;
     total += s;
     if (lane == i) mine = s, idx = best, bits = bb;
   }
@@ -191,8 +210,7 @@ __device__ void place(const ScoredArgs& a, int first, int n, const int* lkeys, i
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, nkeys = a.E * a.L;
   const uint64_t before = lane == 0 ? 0 : ~0ull >> (64 - lane);
   for (int from = 0; from < n; from += kThreads) {
-    for (int j = tid; j < kWaves * nkeys; j += kThreads) wave_cnt[j / nkeys][j % nkeys] = 0;
-    __syncthreads();
+    for (int j = lane; j < nkeys; j += 64) wave_cnt[wave][j] = 0;
     const bool valid = from + tid < n;
     const int s = first + from + tid;
     const int key = !valid ? 0 : lkeys ? lkeys[s] : a.topk_idx[s] * a.L + a.topk_bits[s] - a.b_min;
@@ -203,6 +221,7 @@ __device__ void place(const ScoredArgs& a, int first, int n, const int* lkeys, i
       same &= key >> bit & 1 ? m : ~m;
     }
     const int rank = __popcll(same & before);
+    wave_handoff();  // (a wave's row is its own)
     if (valid && rank == 0) wave_cnt[wave][key] = __popcll(same);
     __syncthreads();
     if (valid) {
