@@ -19,7 +19,9 @@
 // Bound by the instructions of the one CU that has a row: about 25 a token for its
 // weight, 20 more for the histogram, 5 for a list.  (One row of 32000 in binary32 with
 // top-p: 21.7 us, of which 9 in the histogram; 256 of 131072 in bf16 with all bounds:
-// 77 us, reading them alone 11.)  512 threads a row were slower, 27 and 96 us.
+// 71 us, reading them alone 11; the rows without top-k take longest, 37 us of it for the
+// histogram's pass, one over four loads ahead no less.)  512 threads a row were slower,
+// 27 and 96 us.
 //
 #include "decoder.h"
 
@@ -682,10 +684,12 @@ __global__ __launch_bounds__(kThreads) void sample_kernel(SampleArgs a) {
         if (l >= from) list(l, i);
       });
 #pragma unroll
-      for (int j = 0; j < N; ++j)
+      for (int j = 0; j < N; ++j) {
+        if (j % 4 == 2 && *(volatile int*)&s.n > kList) break;  // they do not fit
         if (j * kThreads + tid < row.chunks)
           row.pick(held[j], row.head + (j * kThreads + tid) * PER,
                    [=](float l) { return l >= from; }, list);
+      }
     } else {
       row.each_in(from, top_l, list);
     }
