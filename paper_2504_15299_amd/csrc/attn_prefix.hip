@@ -7,8 +7,14 @@
 // queries.  A workgroup takes a run of keys for its rows, of the prefix or of one
 // sequence's own tokens, keeps the running maximum m, sum l of exp2(score - m) and
 // value sum O, and leaves them as a part in the workspace; a second kernel joins the
-// parts of each query.  Both kinds of run are in one launch: the prefix's are bound by
-// the matrix units, the own tokens' by memory.
+// parts of each query.  Both kinds of run are in one launch, so that a CU has some of
+// each: the prefix's are bound by their instructions, the own tokens' by what one
+// CU reads (32 query and 8 key heads of 128, bf16, us with the join: 64 sequences of up to
+// 512 own tokens behind 8192 shared 43, without the prefix 23.5, without own tokens 41 at
+// one workgroup a CU; 16 behind 2000 15; 2 of 40 behind 501 9).  A step of 64 shared keys
+// and 64 rows takes 4600 cycles, of which 1000 are matrix products, 1800 with the reads
+// and turns of the values, 1300 the loads and the scores, 600 the exponents, 900 the
+// stores and barriers: two waves a SIMD are all that the registers hold.
 //
 // As in the attention of single sequences,
 //   S (keys x queries) = K Q^T,   O^T (values x queries) = V^T P^T
@@ -19,7 +25,7 @@
 namespace d2moe {
 namespace {
 
-constexpr int kThreads = 256, kWaves = 4, kTurn = 256;
+constexpr int kThreads = 256, kWaves = 4;
 constexpr int kRows = 16;  // queries of a lane column set
 // How far (in units of log2) scores may lie above the reference that they are weighed
 // by: it is the largest score when it is set, and moves only past this, so that most
@@ -505,7 +511,8 @@ __device__ void attend_own(const PrefixArgs& a, typename Run<T, DP, 1, 1>::Lds& 
       [&](int) { return 0x7fffffff; }, rows, a.own_o + part * a.D, a.own_ml + part * 2);
 }
 
-// Both kinds of workgroups in turns of kTurn, one a CU.
+// The prefix's workgroups, which take longest, then the own tokens'.  (In turns of 256
+// 44.3 us for 64 sequences behind 8192 keys, this way 43.8; in turns of 8 54.7.)
 template <typename T, int DP, int CT, int NC>
 __global__ __launch_bounds__(kThreads, DP <= 128 ? 2 : 1) void attn_prefix_kernel(PrefixArgs a) {
   union Lds {
@@ -514,19 +521,10 @@ __global__ __launch_bounds__(kThreads, DP <= 128 ? 2 : 1) void attn_prefix_kerne
   };
   __shared__ Lds lds;
   const int i = blockIdx.x;
-  const int both =
-      (a.shared_groups < a.own_groups ? a.shared_groups : a.own_groups) / kTurn * kTurn;
-  int u = i / (2 * kTurn) * kTurn + i % kTurn;
-  bool shared = i % (2 * kTurn) < kTurn;
-  if (i >= 2 * both) {
-    u = i - both;
-    shared = u < a.shared_groups;
-    if (!shared) u = u - a.shared_groups + both;
-  }
-  if (shared)
-    attend_shared<T, DP, CT, NC>(a, lds.shared, u);
+  if (i < a.shared_groups)
+    attend_shared<T, DP, CT, NC>(a, lds.shared, i);
   else
-    attend_own<T, DP>(a, lds.own, u);
+    attend_own<T, DP>(a, lds.own, i - a.shared_groups);
 }
 
 // Joins the parts of a query, a workgroup each: the prefix's runs, then its own, one
@@ -602,8 +600,13 @@ __global__ __launch_bounds__(kThreads) void attn_prefix_join_kernel(PrefixArgs a
 struct Plan {
   int tile_rows, row_tiles, splits, chunk, head_tiles, own_splits, own_chunk;
 };
+// Workgroups that runs are cut for, one a CU of the prefix's (64 sequences behind 8192
+// keys 44.3 us, with 128 of them 64.5, with 512 48.0; the other way without own tokens,
+// 41.1 and 38.5) and two of the own tokens' (9 sequences of 300, fp32: 11.1 us, with 256
+// 12.1; 1024 gain nothing), and the least keys of a run (16 behind 2000 15.6 us, with 64
+// 19.1, with 256 16.6).
 constexpr int kSharedGroups = 256, kOwnGroups = 512;
-constexpr int kLeastKeys = 128;  // of a run
+constexpr int kLeastKeys = 128;
 constexpr int kMostSplits = 64;
 
 void divide(int keys, int64_t units, int groups, int& splits, int& chunk) {
