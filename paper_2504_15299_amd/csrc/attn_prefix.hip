@@ -4,17 +4,19 @@
 //
 // The queries of all sequences and of one key head are the rows of one product with
 // the prefix's keys, up to 64 at a time, so that a shared key is read once for 64
-// queries.  A workgroup takes a run of keys for its rows, of the prefix or of one
-// sequence's own tokens, keeps the running maximum m, sum l of exp2(score - m) and
+// queries.  A workgroup takes a run of the prefix's keys for its rows, a wave one of a
+// sequence's own tokens; either keeps the running maximum m, sum l of exp2(score - m) and
 // value sum O, and leaves them as a part in the workspace; a second kernel joins the
 // parts of each query.  Both kinds of run are in one launch, so that a CU has some of
 // each: the prefix's are bound by their instructions, the own tokens' by what one
 // CU reads (32 query and 8 key heads of 128, bf16, us with the join: 64 sequences of up to
-// 512 own tokens behind 8192 shared 43, without the prefix 23.5, without own tokens 41 at
+// 512 own tokens behind 8192 shared 44, without the prefix 20.4, without own tokens 40 at
 // one workgroup a CU; 16 behind 2000 15; 2 of 40 behind 501 9).  A step of 64 shared keys
 // and 64 rows takes 4600 cycles, of which 1000 are matrix products, 1800 with the reads
 // and turns of the values, 1300 the loads and the scores, 600 the exponents, 900 the
-// stores and barriers: two waves a SIMD are all that the registers hold.
+// stores and barriers: two waves a SIMD are all that the registers hold.  Own tokens by
+// whole workgroups, four waves to a run, joined in LDS, took 23.3 us for 20.4, and 52 for
+// 32 where many have few (114 sequences of up to 39, 64 and 8 heads of 256).
 //
 // As in the attention of single sequences,
 //   S (keys x queries) = K Q^T,   O^T (values x queries) = V^T P^T
@@ -42,7 +44,7 @@ struct PrefixArgs {
   float scale_log2;  // scale / ln 2
   int row_tiles, splits, chunk;           // of the prefix: row tiles, runs of `chunk` keys
   int head_tiles, own_splits, own_chunk;  // of a sequence's own tokens
-  int shared_groups, own_groups;
+  int shared_groups, own_runs;
   float *shared_o, *shared_ml, *own_o, *own_ml;  // parts: rows of D and of (m, l)
   void* out;
 };
@@ -81,14 +83,14 @@ struct Products<uint16_t, DP> {
       o.f[s] = row && c < D ? *(const u4*)(row + c) : u4{0, 0, 0, 0};
     }
   }
-  template <int CT>
-  __device__ static void scores(f4 (&s)[CT][2], const u4* k, const Q (&q)[CT], int lane) {
+  // key(t, c): chunk 4 c + lane / 16 of row 16 t + lane % 16
+  template <int CT, typename Key>
+  __device__ static void scores(f4 (&s)[CT][2], Key key, const Q (&q)[CT]) {
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
       u4 x[KS];
-      const int row = 16 * t + (lane & 15);
 #pragma unroll
-      for (int c = 0; c < KS; ++c) x[c] = k[row * CPR + ((4 * c + (lane >> 4)) ^ swizzle<CPR>(row))];
+      for (int c = 0; c < KS; ++c) x[c] = key(t, c);
 #pragma unroll
       for (int ct = 0; ct < CT; ++ct) {
         s[ct][t] = f4{0.0f, 0.0f, 0.0f, 0.0f};
@@ -120,24 +122,15 @@ struct Products<uint16_t, DP> {
     typedef __bf16 b2 __attribute__((ext_vector_type(2)));
     return __builtin_bit_cast(uint32_t, __builtin_convertvector((f2{a, b}), b2));
   }
-  template <int CT>
-  __device__ static void values(f4 (&o)[CT][H][VE], const P (&p)[CT], const u4* v, int lane) {
-    const int q = lane >> 4;
+  // value(j, h): the VE values of row key_of(j) from 16 VE h + VE (lane % 16) on
+  typedef uint32_t V __attribute__((ext_vector_type(VE / 2)));
+  template <int CT, typename Value>
+  __device__ static void values(f4 (&o)[CT][H][VE], const P (&p)[CT], Value value) {
 #pragma unroll
     for (int h = 0; h < H; ++h) {
-      uint32_t x[NS][VE / 2];
+      V x[NS];
 #pragma unroll
-      for (int j = 0; j < NS; ++j) {
-        const u4* row = v + key_of(j, q) * CPR;
-        if constexpr (VE == 8) {
-          const u4 w = row[16 * h + (lane & 15)];
-#pragma unroll
-          for (int d = 0; d < 4; ++d) x[j][d] = w[d];
-        } else {
-          const uint2 w = *((const uint2*)row + 16 * h + (lane & 15));
-          x[j][0] = w.x, x[j][1] = w.y;
-        }
-      }
+      for (int j = 0; j < NS; ++j) x[j] = value(j, h);
       // four elements at a time, so that no product waits for the one before it
 #pragma unroll
       for (int i0 = 0; i0 < VE; i0 += 4) {
@@ -173,14 +166,13 @@ struct Products<float, DP> {
       o.f[s] = row && c < D ? *(const f4*)(row + c) : f4{0.0f, 0.0f, 0.0f, 0.0f};
     }
   }
-  template <int CT>
-  __device__ static void scores(f4 (&s)[CT][1], const u4* k, const Q (&q)[CT], int lane) {
+  template <int CT, typename Key>
+  __device__ static void scores(f4 (&s)[CT][1], Key key, const Q (&q)[CT]) {
 #pragma unroll
     for (int ct = 0; ct < CT; ++ct) s[ct][0] = f4{0.0f, 0.0f, 0.0f, 0.0f};
-    const int row = lane & 15;
 #pragma unroll
     for (int c = 0; c < KS; ++c) {
-      const f4 x = __builtin_bit_cast(f4, k[row * CPR + ((4 * c + (lane >> 4)) ^ swizzle<CPR>(row))]);
+      const f4 x = __builtin_bit_cast(f4, key(0, c));
 #pragma unroll
       for (int e = 0; e < 4; ++e)
 #pragma unroll
@@ -197,14 +189,14 @@ struct Products<float, DP> {
 #pragma unroll
     for (int j = 0; j < NS; ++j) o.p[j] = p[j];
   }
-  template <int CT>
-  __device__ static void values(f4 (&o)[CT][H][VE], const P (&p)[CT], const u4* v, int lane) {
-    const int q = lane >> 4;
+  typedef u4 V;
+  template <int CT, typename Value>
+  __device__ static void values(f4 (&o)[CT][H][VE], const P (&p)[CT], Value value) {
 #pragma unroll
-    for (int h = 0; h < H; ++h)
+    for (int j = 0; j < NS; ++j)
 #pragma unroll
-      for (int j = 0; j < NS; ++j) {
-        const f4 x = __builtin_bit_cast(f4, v[key_of(j, q) * CPR + 16 * h + (lane & 15)]);
+      for (int h = 0; h < H; ++h) {
+        const f4 x = __builtin_bit_cast(f4, value(j, h));
 #pragma unroll
         for (int i = 0; i < VE; ++i)
 #pragma unroll
@@ -212,6 +204,64 @@ struct Products<float, DP> {
       }
   }
 };
+
+// A tile's scores to the weights of its values: in units of log2, less the reference m;
+// above kRoom the reference moves, and l and o with it.  Where `masks`, masked(ct, key)
+// says which of a lane's are none.
+template <typename M, int CT, typename Masked>
+__device__ inline void weigh(typename M::P (&p)[CT], const f4 (&sc)[CT][M::NS / 4], float scale,
+                             float (&m)[CT], float (&l)[CT], f4 (&o)[CT][M::H][M::VE], bool masks,
+                             Masked masked, int q) {
+  float x[CT][M::NS], mx[CT];
+  bool moves = false;
+#pragma unroll
+  for (int ct = 0; ct < CT; ++ct) {
+    const float ref = m[ct] == -INFINITY ? 0.0f : m[ct];
+#pragma unroll
+    for (int j = 0; j < M::NS; ++j) x[ct][j] = fmaf(sc[ct][j / 4][j % 4], scale, -ref);
+  }
+  if (masks) {
+#pragma unroll
+    for (int ct = 0; ct < CT; ++ct)
+#pragma unroll
+      for (int j = 0; j < M::NS; ++j)
+        if (masked(ct, M::key_of(j, q))) x[ct][j] = -INFINITY;
+  }
+#pragma unroll
+  for (int ct = 0; ct < CT; ++ct) {
+    mx[ct] = -INFINITY;
+#pragma unroll
+    for (int j = 0; j < M::NS; ++j) mx[ct] = fmaxf(mx[ct], x[ct][j]);
+    moves |= mx[ct] > (m[ct] == -INFINITY ? -INFINITY : kRoom);
+  }
+  if (__any(moves)) {
+#pragma unroll
+    for (int ct = 0; ct < CT; ++ct) {
+      mx[ct] = fmaxf(mx[ct], __shfl_xor(mx[ct], 16, 64));
+      mx[ct] = fmaxf(mx[ct], __shfl_xor(mx[ct], 32, 64));
+      // the largest score so far, where there is one
+      const float ref = m[ct] == -INFINITY ? 0.0f : m[ct], top = fmaxf(m[ct], ref + mx[ct]);
+      const float by = top == -INFINITY ? 0.0f : top - ref, alpha = fast_exp2(m[ct] - ref - by);
+      m[ct] = top;
+      l[ct] *= alpha;
+#pragma unroll
+      for (int j = 0; j < M::NS; ++j) x[ct][j] -= by;
+#pragma unroll
+      for (int h = 0; h < M::H; ++h)
+#pragma unroll
+        for (int i = 0; i < M::VE; ++i) o[ct][h][i] *= alpha;
+    }
+  }
+#pragma unroll
+  for (int ct = 0; ct < CT; ++ct) {
+#pragma unroll
+    for (int j = 0; j < M::NS; ++j) {
+      x[ct][j] = fast_exp2(x[ct][j]);
+      l[ct] += x[ct][j];
+    }
+    M::split(p[ct], x[ct]);
+  }
+}
 
 // A run's division among the waves: NC of them share a tile of keys, CT column sets
 // each, the others (kWaves / NC key groups) take other tiles of the same step.
@@ -351,63 +401,21 @@ __device__ void attend(const PrefixArgs& a, typename Run<T, DP, CT, NC>::Lds& ld
     const uint32_t none = (uint32_t)__ballot(
         lds.step.off[span & 1][s % kPer * R::KEYS + kg * M::TK + (lane & (M::TK - 1))] < 0);
     f4 sc[CT][M::NS / 4];
-    M::scores(sc, lds.step.k + kg * M::TK * CPR, qf, lane);
+    const u4* kt = lds.step.k + kg * M::TK * CPR;
+    M::scores(sc, [&](int t, int c) {
+      const int row = 16 * t + col;
+      return kt[row * CPR + ((4 * c + q) ^ swizzle<CPR>(row))];
+    }, qf);
     const int first = k0 + s * R::KEYS + kg * M::TK;
     const bool border = __any(first + M::TK > least);
-    // scores in units of log2, less the reference m; above kRoom the reference moves
-    float x[CT][M::NS], mx[CT];
-    bool moves = false;
-#pragma unroll
-    for (int ct = 0; ct < CT; ++ct) {
-      const float ref = m[ct] == -INFINITY ? 0.0f : m[ct];
-#pragma unroll
-      for (int j = 0; j < M::NS; ++j) x[ct][j] = fmaf(sc[ct][j / 4][j % 4], a.scale_log2, -ref);
-    }
-    if (none != 0 || border) {
-#pragma unroll
-      for (int ct = 0; ct < CT; ++ct)
-#pragma unroll
-        for (int j = 0; j < M::NS; ++j) {
-          const int key = M::key_of(j, q);
-          if ((none >> key & 1) || first + key >= limit[ct]) x[ct][j] = -INFINITY;
-        }
-    }
-#pragma unroll
-    for (int ct = 0; ct < CT; ++ct) {
-      mx[ct] = -INFINITY;
-#pragma unroll
-      for (int j = 0; j < M::NS; ++j) mx[ct] = fmaxf(mx[ct], x[ct][j]);
-      moves |= mx[ct] > (m[ct] == -INFINITY ? -INFINITY : kRoom);
-    }
-    if (__any(moves)) {
-#pragma unroll
-      for (int ct = 0; ct < CT; ++ct) {
-        mx[ct] = fmaxf(mx[ct], __shfl_xor(mx[ct], 16, 64));
-        mx[ct] = fmaxf(mx[ct], __shfl_xor(mx[ct], 32, 64));
-        // the largest score so far, where there is one
-        const float ref = m[ct] == -INFINITY ? 0.0f : m[ct], top = fmaxf(m[ct], ref + mx[ct]);
-        const float by = top == -INFINITY ? 0.0f : top - ref, alpha = fast_exp2(m[ct] - ref - by);
-        m[ct] = top;
-        l[ct] *= alpha;
-#pragma unroll
-        for (int j = 0; j < M::NS; ++j) x[ct][j] -= by;
-#pragma unroll
-        for (int h = 0; h < M::H; ++h)
-#pragma unroll
-          for (int i = 0; i < M::VE; ++i) o[ct][h][i] *= alpha;
-      }
-    }
     typename M::P p[CT];
-#pragma unroll
-    for (int ct = 0; ct < CT; ++ct) {
-#pragma unroll
-      for (int j = 0; j < M::NS; ++j) {
-        x[ct][j] = fast_exp2(x[ct][j]);
-        l[ct] += x[ct][j];
-      }
-      M::split(p[ct], x[ct]);
-    }
-    M::values(o, p, lds.step.v + kg * M::TK * CPR, lane);
+    weigh<M>(p, sc, a.scale_log2, m, l, o, none != 0 || border, [&](int ct, int key) {
+      return (none >> key & 1) || first + key >= limit[ct];
+    }, q);
+    const u4* vt = lds.step.v + kg * M::TK * CPR;
+    M::values(o, p, [&](int j, int h) {
+      return ((const typename M::V*)(vt + M::key_of(j, q) * CPR))[16 * h + col];
+    });
   }
 
   // join the key groups: every row's m, l and O
@@ -490,41 +498,159 @@ __device__ void attend_shared(const PrefixArgs& a, typename Run<T, DP, CT, NC>::
       a.shared_o + part * a.D, a.shared_ml + part * 2);
 }
 
-// A sequence's own tokens, 16 query heads of a key head at a time.
+// A run of a sequence's own tokens by one wave, up to 16 query heads of a key head, which
+// waits for no other: tiles of TK keys, keys through LDS for whole rows' loads, values from
+// memory to the products' registers, the next tile's while this one is weighed.  Row offsets
+// go through LDS a tile ahead, their block-table entries two.
 template <typename T, int DP>
-__device__ void attend_own(const PrefixArgs& a, typename Run<T, DP, 1, 1>::Lds& lds, int u) {
-  const int v = a.by_heads.div(u), hk = u - v * a.H;
-  const int w = a.by_head_tiles.div(v), tile = v - w * a.head_tiles;
+struct OwnLds {
+  int64_t off[2][Products<T, DP>::TK];
+  u4 k[Products<T, DP>::TK * Products<T, DP>::CPR];
+};
+template <typename T, int DP>
+__device__ void attend_own(const PrefixArgs& a, OwnLds<T, DP>& lds, int u) {
+  using M = Products<T, DP>;
+  constexpr int TK = M::TK, CPR = M::CPR, EACH = TK * CPR / 64;
+  const int lane = threadIdx.x & 63, col = lane & 15, q = lane >> 4;
+  const int x = a.by_heads.div(u), hk = u - x * a.H;
+  const int w = a.by_head_tiles.div(x), tile = x - w * a.head_tiles;
   const int split = a.by_seqs.div(w), b = w - split * a.B;
   const int g0 = tile * kRows, rows = a.G - g0 < kRows ? a.G - g0 : kRows;
-  const int from = shared_end(a, b), end = own_end(a, b);
-  const int64_t k0 = from + (int64_t)split * a.own_chunk;
-  const int k1 = split + 1 < a.own_splits && k0 + a.own_chunk < end ? (int)k0 + a.own_chunk : end;
   const int64_t part = (int64_t)u * (a.G < kRows ? a.G : kRows);
-  attend<T, DP, 1, 1>(
-      a, lds, a.table + (int64_t)b * a.max_pages, a.max_pages, hk,
-      k0 < 0x7fffffff ? (int)k0 : 0x7fffffff, k1,
-      [&](int r) -> const T* {
-        return r < rows ? (const T*)a.q + b * a.q_stride + (int64_t)(hk * a.G + g0 + r) * a.D
-                        : nullptr;
-      },
-      [&](int) { return 0x7fffffff; }, rows, a.own_o + part * a.D, a.own_ml + part * 2);
+  float* part_ml = a.own_ml + part * 2;
+  const int from = shared_end(a, b), end = own_end(a, b);
+  const int64_t first = from + (int64_t)split * a.own_chunk;
+  const int k1 = split + 1 < a.own_splits && first + a.own_chunk < end ? (int)first + a.own_chunk
+                                                                       : end;
+  if (k1 <= first) {
+    if (lane < rows) *(float2*)(part_ml + 2 * lane) = make_float2(-INFINITY, 0.0f);
+    return;
+  }
+  const int k0 = (int)first, tiles = (k1 - k0 + TK - 1) / TK;
+  const int32_t* table = a.table + (int64_t)b * a.max_pages;
+  const T* kc = (const T*)a.k + hk * a.head_stride;
+  const T* vc = (const T*)a.v + hk * a.head_stride;
+  int page;
+  auto fetch = [&](int t) {
+    const uint32_t at = a.page.div(k0 + t * TK + (lane & (TK - 1)));
+    page = table[at < (uint32_t)a.max_pages ? at : (uint32_t)a.max_pages - 1];
+  };
+  auto put = [&](int t) {  // returns which are none
+    const uint32_t key = k0 + t * TK + (lane & (TK - 1));
+    const bool in = key < (uint32_t)k1 && (uint32_t)page < (uint32_t)a.n_pages;
+    if (lane < TK)
+      lds.off[t & 1][lane] = in ? page * a.page_stride +
+                                  (int64_t)(key - a.page.div(key) * a.page.d) * a.token_stride
+                            : 0;  // whatever row where there is no key
+    return (uint32_t)__ballot(!in);
+  };
+  fetch(0);
+  typename M::Q qf[1];
+  M::load_q(qf[0],
+            col < rows ? (const T*)a.q + b * a.q_stride + (int64_t)(hk * a.G + g0 + col) * a.D
+                       : nullptr,
+            q, a.D);
+  // chunk e of this lane: row (64 e + lane) / CPR of the tile, chunk lane % CPR; chunks
+  // past the head's end are zero
+  const int c = lane % CPR;
+  const bool wide = c * M::PER < a.D;
+  u4 kf[EACH];
+  typename M::V vf[M::NS][M::H];
+#pragma unroll
+  for (int e = 0; e < EACH; ++e) kf[e] = u4{0, 0, 0, 0};
+  auto load_k = [&](int t) {
+    int64_t at[EACH];
+#pragma unroll
+    for (int e = 0; e < EACH; ++e) at[e] = lds.off[t & 1][(64 * e + lane) / CPR] + c * M::PER;
+    if (wide) {
+#pragma unroll
+      for (int e = 0; e < EACH; ++e) kf[e] = *(const u4*)(kc + at[e]);
+    }
+  };
+  auto load_v = [&](int t) {
+#pragma unroll
+    for (int j = 0; j < M::NS; ++j) {
+      const T* row = vc + lds.off[t & 1][M::key_of(j, q)];
+#pragma unroll
+      for (int h = 0; h < M::H; ++h) {  // (products past the head's end are not used)
+        const int d = M::VE * (16 * h + col);
+        vf[j][h] = *(const typename M::V*)(row + (d < a.D ? d : 0));
+      }
+    }
+  };
+  uint32_t none = put(0);
+  if (tiles > 1) fetch(1);
+  wave_handoff();
+  load_k(0);
+  load_v(0);
+  float m[1] = {-INFINITY}, l[1] = {0.0f};
+  f4 o[1][M::H][M::VE];
+#pragma unroll
+  for (int h = 0; h < M::H; ++h)
+#pragma unroll
+    for (int i = 0; i < M::VE; ++i) o[0][h][i] = f4{0.0f, 0.0f, 0.0f, 0.0f};
+  for (int t = 0; t < tiles; ++t) {
+#pragma unroll
+    for (int e = 0; e < EACH; ++e) {
+      const int row = (64 * e + lane) / CPR;
+      lds.k[row * CPR + (c ^ swizzle<CPR>(row))] = kf[e];
+    }
+    const uint32_t now = none;
+    if (t + 1 < tiles) none = put(t + 1);
+    wave_handoff();
+    if (t + 1 < tiles) load_k(t + 1);
+    if (t + 2 < tiles) fetch(t + 2);
+    f4 sc[1][M::NS / 4];
+    M::scores(sc, [&](int i, int x) {
+      const int row = 16 * i + col;
+      return lds.k[row * CPR + ((4 * x + q) ^ swizzle<CPR>(row))];
+    }, qf);
+    wave_handoff();  // the tile's keys have been read
+    typename M::P p[1];
+    weigh<M>(p, sc, a.scale_log2, m, l, o, now != 0,
+             [&](int, int key) { return now >> key & 1; }, q);
+    if (now != 0) {  // 0 times what a masked row holds is not 0
+#pragma unroll
+      for (int j = 0; j < M::NS; ++j)
+        if (now >> M::key_of(j, q) & 1)
+#pragma unroll
+          for (int h = 0; h < M::H; ++h) vf[j][h] = typename M::V{};
+    }
+    M::values(o, p, [&](int j, int h) { return vf[j][h]; });
+    if (t + 1 < tiles) load_v(t + 1);
+  }
+  l[0] += __shfl_xor(l[0], 16, 64);
+  l[0] += __shfl_xor(l[0], 32, 64);
+  if (col >= rows) return;
+  if (q == 0) *(float2*)(part_ml + 2 * col) = make_float2(m[0], l[0]);
+  float* row = a.own_o + (part + col) * a.D;
+#pragma unroll
+  for (int h = 0; h < M::H; ++h)
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+#pragma unroll
+      for (int i = 0; i < M::VE; i += 4) {
+        const int d = 16 * M::VE * h + M::VE * (4 * q + e) + i;
+        if (d < a.D)
+          *(f4*)(row + d) = f4{o[0][h][i][e], o[0][h][i + 1][e], o[0][h][i + 2][e], o[0][h][i + 3][e]};
+      }
 }
 
-// The prefix's workgroups, which take longest, then the own tokens'.  (In turns of 256
-// 44.3 us for 64 sequences behind 8192 keys, this way 43.8; in turns of 8 54.7.)
+// The prefix's workgroups, which take longest, then the own tokens'.
 template <typename T, int DP, int CT, int NC>
 __global__ __launch_bounds__(kThreads, DP <= 128 ? 2 : 1) void attn_prefix_kernel(PrefixArgs a) {
   union Lds {
     typename Run<T, DP, CT, NC>::Lds shared;
-    typename Run<T, DP, 1, 1>::Lds own;
+    OwnLds<T, DP> own[kWaves];
   };
   __shared__ Lds lds;
-  const int i = blockIdx.x;
-  if (i < a.shared_groups)
-    attend_shared<T, DP, CT, NC>(a, lds.shared, i);
-  else
-    attend_own<T, DP>(a, lds.own, i - a.shared_groups);
+  if ((int)blockIdx.x < a.shared_groups) {
+    attend_shared<T, DP, CT, NC>(a, lds.shared, blockIdx.x);
+  } else {
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int u = (blockIdx.x - a.shared_groups) * kWaves + wave;
+    if (u < a.own_runs) attend_own<T, DP>(a, lds.own[wave], u);
+  }
 }
 
 // Joins the parts of a query, a workgroup each: the prefix's runs, then its own, one
@@ -600,23 +726,25 @@ __global__ __launch_bounds__(kThreads) void attn_prefix_join_kernel(PrefixArgs a
 struct Plan {
   int tile_rows, row_tiles, splits, chunk, head_tiles, own_splits, own_chunk;
 };
-// Workgroups that runs are cut for, one a CU of the prefix's (64 sequences behind 8192
-// keys 44.3 us, with 128 of them 64.5, with 512 48.0; the other way without own tokens,
-// 41.1 and 38.5) and two of the own tokens' (9 sequences of 300, fp32: 11.1 us, with 256
-// 12.1; 1024 gain nothing), and the least keys of a run (16 behind 2000 15.6 us, with 64
-// 19.1, with 256 16.6).
-constexpr int kSharedGroups = 256, kOwnGroups = 512;
-constexpr int kLeastKeys = 128;
+// Runs that the keys are cut into: of the prefix's one a CU (64 sequences behind 8192
+// keys 44 us, with 128 of them 64, with 512 48; the other way without own tokens, 40 and
+// 36), of the own tokens eight a CU (64 sequences of up to 512, 12 heads of 64 in fp32: 30.0
+// us, with 1024 of them 37.4; 4096 take 22.7 for 20.4 with 32 and 8 heads of 128 in bf16);
+// and the least keys of a run (of the prefix: 16 sequences behind 2000 15.6 us, with 64
+// 19.1, with 256 16.6; of the own tokens: 9 of 300 behind 1500, fp32, 10.9 us, with 128
+// 13.9; 32 of 300 with heads of 256 47.5, with 32 53.6).
+constexpr int kSharedGroups = 256, kOwnRuns = 2048;
+constexpr int kLeastKeys = 128, kLeastOwn = 64;
 constexpr int kMostSplits = 64;
 
-void divide(int keys, int64_t units, int groups, int& splits, int& chunk) {
+void divide(int keys, int64_t units, int groups, int least, int& splits, int& chunk) {
   int64_t most = units >= groups ? 1 : groups / units;
   most = most < kMostSplits ? most : kMostSplits;
-  const int64_t need = ((int64_t)keys + kLeastKeys - 1) / kLeastKeys;
+  const int64_t need = ((int64_t)keys + least - 1) / least;
   splits = (int)(need < most ? need : most);
   if (splits < 1) splits = 1;
   chunk = (int)(((int64_t)keys + splits - 1) / splits + 31) / 32 * 32;
-  if (chunk < kLeastKeys) chunk = kLeastKeys;
+  if (chunk < least) chunk = least;
 }
 
 Plan plan_of(int B, int q_heads, int n_heads, int max_prefix, int max_rest) {
@@ -625,8 +753,8 @@ Plan plan_of(int B, int q_heads, int n_heads, int max_prefix, int max_rest) {
   p.tile_rows = rows <= 16 ? 16 : rows <= 32 ? 32 : 64;
   p.row_tiles = (rows + p.tile_rows - 1) / p.tile_rows;
   p.head_tiles = (G + kRows - 1) / kRows;
-  divide(max_prefix, (int64_t)n_heads * p.row_tiles, kSharedGroups, p.splits, p.chunk);
-  divide(max_rest, (int64_t)n_heads * p.head_tiles * B, kOwnGroups, p.own_splits, p.own_chunk);
+  divide(max_prefix, (int64_t)n_heads * p.row_tiles, kSharedGroups, kLeastKeys, p.splits, p.chunk);
+  divide(max_rest, (int64_t)n_heads * p.head_tiles * B, kOwnRuns, kLeastOwn, p.own_splits, p.own_chunk);
   return p;
 }
 int64_t shared_rows(const Plan& p, int n_heads) {
@@ -639,7 +767,7 @@ int64_t own_rows(const Plan& p, int B, int q_heads, int n_heads) {
 
 template <typename T, int DP>
 hipError_t run_prefix_d(const PrefixArgs& a, int tile_rows, hipStream_t s) {
-  const int grid = a.shared_groups + a.own_groups;
+  const int grid = a.shared_groups + (a.own_runs + kWaves - 1) / kWaves;
   if (tile_rows == 16)
     attn_prefix_kernel<T, DP, 1, 1><<<grid, kThreads, 0, s>>>(a);
   else if (tile_rows == 32)
@@ -691,7 +819,7 @@ hipError_t launch_attn_prefix(const void* q, int64_t q_stride, int B, int q_head
   a.row_tiles = p.row_tiles, a.splits = p.splits, a.chunk = p.chunk;
   a.head_tiles = p.head_tiles, a.own_splits = p.own_splits, a.own_chunk = p.own_chunk;
   a.shared_groups = c->n_heads * p.row_tiles * p.splits;
-  a.own_groups = c->n_heads * p.head_tiles * B * p.own_splits;
+  a.own_runs = c->n_heads * p.head_tiles * B * p.own_splits;
   const int64_t rows = shared_rows(p, c->n_heads), own = own_rows(p, B, q_heads, c->n_heads);
   a.shared_o = (float*)ws, a.own_o = a.shared_o + rows * a.D;
   a.shared_ml = a.own_o + own * a.D, a.own_ml = a.shared_ml + rows * 2;
