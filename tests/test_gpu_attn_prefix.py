@@ -224,6 +224,38 @@ def test_prefix_past_32_bit_offsets():
     assert torch.equal(got, api.attn_prefix(q, small, table, lengths, ptab, shared))
 
 
+@pytest.mark.parametrize("Hq,H", [(1, 1), (34, 2)])
+def test_the_most_sequences(Hq, H):
+    """65535 sequences behind three shared tokens, each with one or no token of its own in
+    pages of one token, and two tiles of heads where there are 17 to a key head."""
+    B, D, G = 65535, 8, Hq // H
+    torch.manual_seed(Hq)
+    cache = api.KVCache.empty(B + 3, 1, H, D, F32, DEV)
+    cache.k.normal_()
+    cache.v.normal_()
+    q = torch.randn((B, Hq, D), device=DEV)
+    order = torch.randperm(B + 3, device=DEV).to(I32)
+    table = torch.full((B, 4), -1, dtype=I32, device=DEV)
+    table[:, 3] = order[3:]
+    lengths = 3 + (torch.arange(B, device=DEV) % 3 > 0).to(I32)
+    out = api.attn_prefix(q, cache, table, lengths, order[:3].contiguous(),
+                          torch.full((B,), 3, dtype=I32, device=DEV))
+    at = order.long()
+    k, v = (torch.cat([t[at[:3], 0].double().expand(B, 3, H, D), t[at[3:], 0].double()[:, None]], 1)
+            .permute(0, 2, 1, 3) for t in (cache.k, cache.v))
+    x = q.double().view(B, H, G, 1, D)
+    s = (x * k[:, :, None]).sum(-1) * D ** -0.5
+    s[lengths == 3, :, :, 3] = -float("inf")
+    p = torch.softmax(s, -1)
+    want = (p[..., None] * v[:, :, None]).sum(3).view(B, Hq, D)
+    # scores of 8 products: off by 9 2^-24 of the sum of |products|; a weight by twice that, the
+    # exponents' own 2^-22, the joins' products and the sums of 4 keys
+    ds = 9 * 2.0 ** -24 * (x * k[:, :, None]).abs().sum(-1).amax(-1) * D ** -0.5
+    mag = (p[..., None] * v[:, :, None].abs()).sum(3)
+    err = mag * (2 * ds[..., None] + 2.0 ** -20)
+    assert ((out.double() - want).abs() <= err.view(B, Hq, D)).all()
+
+
 def test_graphs_over_one_workspace_and_another_stream():
     """Two captured calls over one workspace, replayed in turn with eager work between,
     follow their lengths, shares and queries."""
