@@ -240,8 +240,8 @@ d2moe_status d2moe_route_learned(const void* x, d2moe_dtype x_dtype, int32_t T,
  * Scores, sums and comparisons are binary64.  A logit of -infinity has a score of 0; a
  * softmax over nothing else gives scores of 0, and scores that sum to 0 give weights of
  * 0; logits of +infinity share a softmax's whole.  An expert with a NaN is chosen last
- * (its own score is NaN, the others' do not depend on it).  Bit-widths, counts, scan, permutation and flags are those of
- * d2moe_route.
+ * (its own score is NaN, the others' do not depend on it).  Bit-widths, counts, scan,
+ * permutation and flags are those of d2moe_route.
  *   select_bias: device [E] float or NULL (zeros)
  * 1 <= k <= top_groups * (E / groups), E % groups == 0, E <= 64, scale finite.
  */

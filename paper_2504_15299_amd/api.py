@@ -110,8 +110,8 @@ def lib():
         L.d2moe_linear_forward.argtypes = [_P, _I, _I, lin, _P, _P, _I, _P]
         L.d2moe_kv_append.argtypes = [_P, i64, _I, _P, _P, i64, _I, _I, kvc, _P, _I, _I, _P, _P,
                                       _P, _P, _I, _P, _P]
-        L.d2moe_kv_append_norm.argtypes = [_P, i64, _I, _P, _P, i64, _I, _I, kvc, _P, _I, _I, _P, _P,
-                                           _P, _P, f32, _P, _P, _I, _I, _I, _P, _P]
+        L.d2moe_kv_append_norm.argtypes = [_P, i64, _I, _P, _P, i64, _I, _I, kvc, _P, _I, _I, _P,
+                                           _P, _P, _P, f32, _P, _P, _I, _I, _I, _P, _P]
         L.d2moe_attn_decode_workspace.argtypes = [_I, _I, _I, _I, _I, sz]
         L.d2moe_attn_decode.argtypes = [_P, i64, _I, _I, kvc, _P, _I, _P, _I, _I, f32, _P, _P,
                                         size, _P]
@@ -386,8 +386,8 @@ def route_scored(logits, k: int, token_req, bit_table: torch.Tensor, scoring: st
     if logits is None:
         pl = _arg(out.logits, (T, E), f32, dev, "logits")
     elif out.logits is not logits:
-        out = Routing(logits, out.topk_idx, out.topk_w, out.topk_bits, out.hist, out.offsets, out.perm,
-                      out.slot_of, out.expert_maxbit, out.flags)
+        out = Routing(logits, out.topk_idx, out.topk_w, out.topk_bits, out.hist, out.offsets,
+                      out.perm, out.slot_of, out.expert_maxbit, out.flags)
     c = _Routing(pl, _arg(out.topk_idx, (T, k), i32, dev, "topk_idx"),
                  _arg(out.topk_w, (T, k), f32, dev, "topk_w"),
                  _arg(out.topk_bits, (T, k), u8, dev, "topk_bits"),

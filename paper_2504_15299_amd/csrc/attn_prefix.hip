@@ -632,7 +632,8 @@ __device__ void attend_own(const PrefixArgs& a, OwnLds<T, DP>& lds, int u) {
       for (int i = 0; i < M::VE; i += 4) {
         const int d = 16 * M::VE * h + M::VE * (4 * q + e) + i;
         if (d < a.D)
-          *(f4*)(row + d) = f4{o[0][h][i][e], o[0][h][i + 1][e], o[0][h][i + 2][e], o[0][h][i + 3][e]};
+          *(f4*)(row + d) = f4{o[0][h][i][e], o[0][h][i + 1][e], o[0][h][i + 2][e],
+                               o[0][h][i + 3][e]};
       }
 }
 
@@ -663,7 +664,8 @@ __global__ __launch_bounds__(kThreads) void attn_prefix_join_kernel(PrefixArgs a
   __shared__ __align__(16) f4 po[kSubs][LANES];
   const int head = blockIdx.x, b = blockIdx.y;
   const int hk = head / a.G, g = head - hk * a.G;
-  const int sub = threadIdx.x / LANES, lane = threadIdx.x % LANES, d = 4 * lane < a.D ? 4 * lane : 0;
+  const int sub = threadIdx.x / LANES, lane = threadIdx.x % LANES;
+  const int d = 4 * lane < a.D ? 4 * lane : 0;
   const int own_rows = a.G < kRows ? a.G : kRows;
   const int r = b * a.G + g, tile = r / tile_rows, n = a.splits + a.own_splits;
   float mm = -INFINITY, ll = 0.0f;
@@ -680,7 +682,8 @@ __global__ __launch_bounds__(kThreads) void attn_prefix_join_kernel(PrefixArgs a
             (((int64_t)i * a.row_tiles + tile) * a.H + hk) * tile_rows + r % tile_rows;
         o = a.shared_o + p * a.D, m = a.shared_ml + p * 2;
       } else {
-        const int64_t u = (((int64_t)(i - a.splits) * a.B + b) * a.head_tiles + g / kRows) * a.H + hk;
+        const int64_t w = ((int64_t)(i - a.splits) * a.B + b) * a.head_tiles + g / kRows;
+        const int64_t u = w * a.H + hk;
         const int64_t p = u * own_rows + g % kRows;
         o = a.own_o + p * a.D, m = a.own_ml + p * 2;
       }
@@ -754,7 +757,8 @@ Plan plan_of(int B, int q_heads, int n_heads, int max_prefix, int max_rest) {
   p.row_tiles = (rows + p.tile_rows - 1) / p.tile_rows;
   p.head_tiles = (G + kRows - 1) / kRows;
   divide(max_prefix, (int64_t)n_heads * p.row_tiles, kSharedGroups, kLeastKeys, p.splits, p.chunk);
-  divide(max_rest, (int64_t)n_heads * p.head_tiles * B, kOwnRuns, kLeastOwn, p.own_splits, p.own_chunk);
+  divide(max_rest, (int64_t)n_heads * p.head_tiles * B, kOwnRuns, kLeastOwn, p.own_splits,
+         p.own_chunk);
   return p;
 }
 int64_t shared_rows(const Plan& p, int n_heads) {

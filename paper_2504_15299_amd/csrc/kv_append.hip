@@ -167,7 +167,8 @@ __device__ inline void turn_pair(float& a, float& b, float cos, float sin) {
 template <typename TI, typename TO, int N, int LANES>
 __global__ __launch_bounds__(kAppendThreads, kNormGroups) void kv_append_norm_kernel(NormArgs g) {
   typedef Words<Pack<TI, N>> W;
-  constexpr int kHeads = 64 / LANES, kWaves = kAppendThreads / 64;  // (heads side by side in a wave)
+  constexpr int kHeads = 64 / LANES;  // side by side in a wave
+  constexpr int kWaves = kAppendThreads / 64;
   const AppendArgs& a = g.a;
   const int lane = threadIdx.x & 63, l = lane & (LANES - 1);
   const int pairs = g.R / 2;          // of a head

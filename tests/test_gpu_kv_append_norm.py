@@ -182,3 +182,23 @@ def test_another_stream():
     got = api.kv_append_norm(*a, q_weight=w, stream=s)
     torch.cuda.synchronize()
     assert torch.equal(got, want)
+
+
+def test_pages_past_32_bit_offsets():
+    """Pages behind the first 2^31 elements of the cache take what those of a small one do."""
+    H, Hq, D, page = 2, 4, 128, 16
+    n = (1 << 31) // (page * H * D) + 10
+    torch.manual_seed(1)
+    qkv = torch.randn((6, Hq + 2 * H, D), device=DEV).to(BF)
+    w, table = torch.rand(D, device=DEV), torch.tensor([[3, 0], [5, 7]], dtype=I32, device=DEV)
+    pos = torch.tensor([0, 15, 31, 3, 4, 20], dtype=I32, device=DEV)
+    seq = torch.tensor([0, 0, 0, 1, 1, 1], dtype=I32, device=DEV)
+    got = []
+    for pages, off in ((n, n - 8), (8, 0)):
+        c = api.KVCache(*(torch.zeros((pages, page, H, D), dtype=BF, device=DEV) for _ in range(2)))
+        q = api.kv_append_norm(qkv[:, :Hq], qkv[:, Hq:Hq + H], qkv[:, Hq + H:], c, table + off, pos,
+                               seq, q_weight=w, k_weight=w)
+        got.append((q, c.k[off:].clone(), c.v[off:].clone(), c.k[:off].any().item()))
+    for a, b in zip(got[0][:3], got[1][:3]):
+        assert torch.equal(a, b)
+    assert not got[0][3] and got[1][1].any()
