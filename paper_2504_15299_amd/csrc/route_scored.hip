@@ -12,7 +12,7 @@
 // token chooses, then every kBlock slots are counted, each key's counts scanned over the
 // blocks, and the slots placed; the tables between the launches lie in the part of
 // slot_of that their block writes last.  8192 tokens, 6 of 64 experts in 4 of 8 groups,
-// sigmoid: 9.3 + 2.8 + 3.1 + 5.1 us, the choice bound by its instructions (3 MB cross
+// sigmoid: 9.3 + 2.8 + 3.0 + 4.8 us, the choice bound by its instructions (3 MB cross
 // the memory, 0.6 us), the others by latency.
 #include "internal.h"
 
@@ -203,9 +203,13 @@ __device__ inline void scan_keys(const int* cnt, int* off, int nkeys, int lane) 
   if (lane == 63) off[nkeys] = acc;
 }
 
+__device__ inline int key_of(const ScoredArgs& a, int s) {
+  return a.topk_idx[s] * a.L + a.topk_bits[s] - a.b_min;
+}
+
 // perm and slot_of of slots first .. first + n - 1, in slot order within a key, key j's
-// from base[j] on (which moves on).
-__device__ void place(const ScoredArgs& a, int first, int n, const int* lkeys, int* base,
+// from base[j] on (which moves on).  mine: the key of slot first + threadIdx.x.
+__device__ void place(const ScoredArgs& a, int first, int n, const int* lkeys, int mine, int* base,
                       int (&wave_cnt)[kWaves][kMaxKeys]) {
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, nkeys = a.E * a.L;
   const uint64_t before = lane == 0 ? 0 : ~0ull >> (64 - lane);
@@ -213,7 +217,7 @@ __device__ void place(const ScoredArgs& a, int first, int n, const int* lkeys, i
     for (int j = lane; j < nkeys; j += 64) wave_cnt[wave][j] = 0;
     const bool valid = from + tid < n;
     const int s = first + from + tid;
-    const int key = !valid ? 0 : lkeys ? lkeys[s] : a.topk_idx[s] * a.L + a.topk_bits[s] - a.b_min;
+    const int key = !valid ? 0 : from == 0 ? mine : lkeys ? lkeys[s] : key_of(a, s);
     uint64_t same = __ballot(valid);
 #pragma unroll
     for (int bit = 0; bit < 9; ++bit) {
@@ -273,7 +277,7 @@ __global__ __launch_bounds__(kThreads) void scored_one_kernel(ScoredArgs a) {
   }
   if (fl) atomicOr(&flag, fl);
   for (int s = tid; s < n; s += kThreads)
-    atomicAdd(&cnt[SELECT ? lkeys[s] : a.topk_idx[s] * a.L + a.topk_bits[s] - a.b_min], 1);
+    atomicAdd(&cnt[SELECT ? lkeys[s] : key_of(a, s)], 1);
   __syncthreads();
   if (wave == 0) scan_keys(cnt, off, nkeys, lane);
   if (tid == 0) *a.flags = flag;
@@ -281,7 +285,8 @@ __global__ __launch_bounds__(kThreads) void scored_one_kernel(ScoredArgs a) {
   for (int j = tid; j < nkeys; j += kThreads) a.hist[j] = cnt[j];
   write_totals(a, cnt, off);
   __syncthreads();
-  place(a, 0, n, SELECT ? lkeys : nullptr, off, wave_cnt);
+  const int mine = tid < n ? SELECT ? lkeys[tid] : key_of(a, tid) : 0;
+  place(a, 0, n, SELECT ? lkeys : nullptr, mine, off, wave_cnt);
 }
 
 // Slots of block b of nb.
@@ -297,7 +302,7 @@ __global__ __launch_bounds__(kThreads) void scored_count_kernel(ScoredArgs a) {
   for (int j = threadIdx.x; j <= nkeys; j += kThreads) cnt[j] = 0;
   __syncthreads();
   for (int s = first + threadIdx.x; s < first + n; s += kThreads) {
-    atomicAdd(&cnt[a.topk_idx[s] * a.L + a.topk_bits[s] - a.b_min], 1);
+    atomicAdd(&cnt[key_of(a, s)], 1);
     if (s < a.T && a.perm[s]) atomicOr(&cnt[nkeys], a.perm[s]);
   }
   __syncthreads();
@@ -337,15 +342,22 @@ __global__ __launch_bounds__(256) void scored_scan_kernel(ScoredArgs a, int nb) 
 __global__ __launch_bounds__(kThreads) void scored_place_kernel(ScoredArgs a) {
   __shared__ int cnt[kMaxKeys], off[kMaxKeys + 1], wave_cnt[kWaves][kMaxKeys];
   const int tid = threadIdx.x, nkeys = a.E * a.L, first = blockIdx.x * kBlock;
-  for (int j = tid; j < nkeys; j += kThreads) cnt[j] = a.hist[j];
+  const int n = block_slots(a, blockIdx.x, gridDim.x);
+  // everything from memory at once (a key a thread)
+  const int count = tid < nkeys ? a.hist[tid] : 0;
+  const int before = tid < nkeys ? a.slot_of[first + tid] : 0;
+  const int mine = tid < n ? key_of(a, first + tid) : 0;
+  if (tid < nkeys) cnt[tid] = count;
   __syncthreads();
   if (tid < 64) scan_keys(cnt, off, nkeys, tid);
+  __syncthreads();  // and the block's part of slot_of has been read
+  if (blockIdx.x == 0) {
+    write_totals(a, cnt, off);
+    __syncthreads();
+  }
+  if (tid < nkeys) off[tid] += before;
   __syncthreads();
-  if (blockIdx.x == 0) write_totals(a, cnt, off);
-  __syncthreads();
-  for (int j = tid; j < nkeys; j += kThreads) off[j] += a.slot_of[first + j];
-  __syncthreads();  // the block's part of slot_of has been read
-  place(a, first, block_slots(a, blockIdx.x, gridDim.x), nullptr, off, wave_cnt);
+  place(a, first, n, nullptr, mine, off, wave_cnt);
 }
 
 }  // namespace
