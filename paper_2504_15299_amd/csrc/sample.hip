@@ -19,7 +19,7 @@
 // Bound by the instructions of the one CU that has a row: about 25 a token for its
 // weight, 20 more for the histogram, 5 for a list.  (One row of 32000 in binary32 with
 // top-p: 21.7 us, of which 9 in the histogram; 256 of 131072 in bf16 with all bounds:
-// 71 us, reading them alone 11; the rows without top-k take longest, 37 us of it for the
+// 71 to 75 us, reading them alone 11; the rows without top-k take longest, 37 us of it for the
 // histogram's pass, one over four loads ahead no less.)  512 threads a row were slower,
 // 27 and 96 us.
 //
