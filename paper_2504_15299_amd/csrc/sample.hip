@@ -546,7 +546,10 @@ __device__ bool select_both(Lds& s, const RowOf<T>& row, const Weights& x, const
   row.each([=](float l) { return (l >= lo_u && l <= hi_u) || (l >= lo_p && l <= hi_p); },
            [&](float l, int i) { append(s, l, i); });
   __syncthreads();
-  if (s.n > kList) return false;
+  if (s.n > kList) {
+    __syncthreads();  // every wave has seen it: the caller's next search empties the list
+    return false;
+  }
   const int n = sort_list(s, x, s.n, bins), i = threadIdx.x;
   // the token's bins come first; the others' sums begin anew where they do not adjoin
   const u64 run = i < n ? s.sums[i] : 0, was = i < n && i > 0 ? s.sums[i - 1] : 0;
