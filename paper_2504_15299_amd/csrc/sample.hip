@@ -23,6 +23,8 @@
 // histogram's pass, one over four loads ahead no less.)  512 threads a row were slower,
 // 27 and 96 us.
 //
+#include <cfloat>
+
 #include "decoder.h"
 
 namespace d2moe {
@@ -191,7 +193,8 @@ struct Weights {
     lo = (float)(a - 1e-6 * fabs(a) - 1e-37);
     hi = (float)(b + 1e-6 * fabs(b) + 1e-37);
     if (!(lo <= hi)) lo = -INFINITY, hi = INFINITY;  // (1 / t is 0)
-    if (bin == kBins - 1) lo = -INFINITY;
+    // -infinity is in no range: it is never drawn, and its key 0 stands for no value
+    lo = bin == kBins - 1 ? -FLT_MAX : fmaxf(lo, -FLT_MAX);
   }
 };
 static_assert(kSteps == 256, "scaled() takes units by a shift of 8");
@@ -427,7 +430,8 @@ __device__ void select(Lds& s, const RowOf<T>& row, const Weights& x, const Pref
     mx = key > mx ? key : mx;
   });
   uint32_t lo = ~block_max(s, mn, turn), hi = block_max(s, mx, turn);
-  while (lo != hi) {
+  // (each time 2^11 times fewer keys: three times at most)
+  for (int round = 0; lo != hi && round < 3; ++round) {
     int shift = 0;
     while ((hi - lo) >> shift >= (uint32_t)kBins) ++shift;
     for (int j = threadIdx.x; j < kBins; j += kThreads) s.count[j] = 0, s.weight[j] = 0;

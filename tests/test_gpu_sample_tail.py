@@ -1,5 +1,7 @@
-"""Tokens whose choice is looked for among more tokens than one list holds, against the
-plain form in binary64."""
+"""Tokens whose choice is looked for among the least weights, or among more tokens than
+one list holds, against the plain form in binary64."""
+import math
+
 import numpy as np
 import pytest
 import torch
@@ -40,3 +42,64 @@ def test_top_p_of_equal_logits(dtype):
     x = torch.zeros((256, 4096), dtype=dtype)
     tokens, probs = api.sample(gpu(x), gpu(u, F32), top_p=gpu([0.5] * 256, F32))
     assert tokens.tolist() == [int(a * 2048) for a in u] and (probs == 2.0 ** -11).all()
+
+
+def temperature_for(row, k):
+    """The temperature at which a row's k-th largest weighs 2^-33.5 of the largest: below
+    2^-31.98 one bin takes all that follows."""
+    d = np.sort(row[row > -1e30].astype(np.float64))[::-1]
+    assert len(row) - k > LIST
+    return (d[0] - d[k - 1]) / (33.5 * math.log(2))
+
+
+@pytest.mark.parametrize("dtype", [F32, BF])
+@pytest.mark.parametrize("mask", [-float("inf"), float("nan"), torch.finfo(BF).min])
+@pytest.mark.parametrize("p,m", [(None, None), (0.9, None), (None, 0.01), (0.7, 0.001)])
+@pytest.mark.parametrize("k", [513, 600, 1500, 12000])
+def test_top_k_among_the_least_weights(k, p, m, mask, dtype):
+    """Half of a vocabulary masked, a low temperature and a top-k that ends far below the
+    largest: the masked tokens are not looked through."""
+    V, B = 32000, 6
+    x = normal(B, V, dtype)
+    x[torch.rand((B, V), generator=torch.Generator().manual_seed(1)) < 0.5] = mask
+    rows = x.float().numpy()
+    t = [temperature_for(r, k) for r in rows]
+    tokens, _ = run(x, np.random.default_rng(k).random(B), t, k, p, m)
+    for b in range(B):
+        assert 0 <= tokens[b] < V and rows[b, tokens[b]] > -100.0
+
+
+@pytest.mark.parametrize("mask", [-float("inf"), float("nan")])
+@pytest.mark.parametrize("p", [1.0 - 2.0 ** -24, 1.0])
+def test_tokens_of_the_least_weights(mask, p):
+    """One large logit, thousands of 2^-33 of its weight and thousands masked: what is
+    drawn past the first is one of the thousands, in the order of their indexes.
+
+    A weight is off by 2^-48 (half a unit) and 2^-42 of itself, so the running sum of n
+    of them by n (2^-15 + 2^-42) of one."""
+    V, n = 32000, 20000
+    g = torch.Generator().manual_seed(3)
+    at = torch.randperm(V, generator=g)[:n].sort().values
+    x = torch.full((V,), mask)
+    x[at] = -33 * math.log(2)
+    first = 17
+    x[first] = 0.0
+    w = math.exp(float(x[at[at != first][0]]))
+    rest = at[at != first].numpy()
+    us = np.array([0.5, 1 - 2.0 ** -23, 1 - 2.0 ** -24], np.float32)
+    tokens, probs = api.sample(gpu(x.expand(3, V).contiguous()), gpu(us),
+                               top_p=gpu([p] * 3, F32))
+    tokens, probs = tokens.tolist(), probs.tolist()
+    whole = 1 + w * len(rest)
+    kept = whole if p == 1.0 else 1 + w * math.ceil((p * whole - 1) / w)
+    assert tokens[0] == first
+    for u, token in zip(us[1:], tokens[1:]):
+        i = int((float(u) * kept - 1) / w) if float(u) * kept >= 1 else -1
+        if i < 0:
+            assert token == first
+            continue
+        near = abs(int(np.searchsorted(rest, token)) - i)
+        assert token in rest and near <= 2 + len(rest) * (2.0 ** -15 + 2.0 ** -42)
+    for token, share in zip(tokens, probs):
+        want = (1.0 if token == first else w) / kept
+        assert abs(share - want) <= (2.0 ** -24 + 2.0 ** -14) * want
