@@ -699,8 +699,9 @@ __global__ __launch_bounds__(kThreads) void attn_prefix_join_kernel(PrefixArgs a
     acc *= was;
 #pragma unroll
     for (int e = 0; e < kAhead; ++e) {
-      // without a key there may be no values written
-      if (i0 + e * kSubs >= n || ml[e].x == -INFINITY) continue;
+      // without a key there may be no values written; scores that are NaN, which no maximum
+      // knows of, have left a sum that is
+      if (i0 + e * kSubs >= n || (ml[e].x == -INFINITY && ml[e].y == 0.0f)) continue;
       const float f = fast_exp2(ml[e].x - mm);
       ll = fmaf(f, ml[e].y, ll);
       acc += f * v[e];
