@@ -100,9 +100,10 @@ __device__ int select(const ScoredArgs& a, int t, int lane, double (&tmp)[64], i
   } else {
     const uint32_t most = wave_max(ordered(x == x ? logit + 0.0f : -INFINITY));
     const double top = __builtin_bit_cast(float, most >> 31 ? most & ~(1u << 31) : ~most);
-    const double e = !have || top == -INFINITY ? 0.0 : x == top ? 1.0 : exp(x - top);
-    const double sum = wave_sum(e == e ? e : 0.0);
-    score = sum == 0.0 ? 0.0 : e / sum;  // nothing but masked logits: no weight at all
+    const double e = x == top ? 1.0 : exp(x - top);
+    const double sum = wave_sum(e == e && top > -INFINITY ? e : 0.0);
+    // nothing but masked logits: no weight at all; a NaN keeps its own
+    score = x == x && sum == 0.0 ? 0.0 : e / sum;
   }
   const double by = have && a.select_bias ? score + (double)a.select_bias[lane] : score;
   bool live = have;
