@@ -652,8 +652,8 @@ d2moe_status d2moe_attn_decode(const void* q, int64_t q_stride, int32_t B, int32
  *        run at the same time need one each
  *   out: packed; may begin where q does, whatever q's stride
  * Everything else as d2moe_attn_decode without a window: lengths, masked tokens, rows
- * without a key, types, sums and limits (also prefix_pages * page_size <= 2^30).  Value
- * rows (not key rows) of tokens attended must be finite: an infinite one may give NaN.
+ * without a key, types, sums and limits (also prefix_pages * page_size <= 2^30).  An
+ * infinite value (not key) may give NaN to the sequences that attend it, to no others.
  */
 d2moe_status d2moe_attn_prefix_workspace(int32_t B, int32_t q_heads, int32_t n_heads,
                                          int32_t head_dim, int32_t max_prefix, int32_t max_rest,

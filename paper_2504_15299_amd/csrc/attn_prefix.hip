@@ -286,6 +286,45 @@ struct Run {
   };
 };
 
+// One row's value sum by a wave, a key after the other and only those that it attends.  In
+// the matrix products 0 times an infinite or NaN value is not 0, so that such a value
+// reaches the rows of a tile that do not attend its key as well: seldom, and their sums are
+// made here once more.
+__device__ inline float value_of(const uint16_t* p) { return bf2f(*p); }
+__device__ inline float value_of(const float* p) { return *p; }
+template <typename T, int DP>
+__device__ void own_sum(const PrefixArgs& a, const int32_t* table, const T* kc, const T* vc,
+                        const T* query, int k0, int k1, float m, float* out) {
+  constexpr int N = DP / 64;  // dimensions of a lane
+  const int lane = threadIdx.x & 63;
+  float q[N], sum[N];
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    sum[i] = 0.0f;
+    q[i] = 64 * i + lane < a.D ? value_of(query + 64 * i + lane) : 0.0f;
+  }
+#pragma unroll 1
+  for (int key = k0; key < k1; ++key) {
+    const uint32_t at = a.page.div(key);
+    const int page = table[at];
+    if ((uint32_t)page >= (uint32_t)a.n_pages) continue;
+    const int64_t off = page * a.page_stride + (int64_t)(key - at * a.page.d) * a.token_stride;
+    float score = 0.0f;
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+      if (64 * i + lane < a.D) score = fmaf(q[i], value_of(kc + off + 64 * i + lane), score);
+#pragma unroll
+    for (int by = 1; by < 64; by *= 2) score += __shfl_xor(score, by, 64);
+    const float w = fast_exp2(fmaf(score, a.scale_log2, -m));
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+      if (64 * i + lane < a.D) sum[i] = fmaf(w, value_of(vc + off + 64 * i + lane), sum[i]);
+  }
+#pragma unroll
+  for (int i = 0; i < N; ++i)
+    if (64 * i + lane < a.D) out[64 * i + lane] = sum[i];
+}
+
 // Keys k0 .. k1 - 1 of `table` (pages of it) and key head hk for the rows of a tile:
 // row(r) is query r, or null; limit(r) the end of the keys that it attends.  Rows 0 ..
 // rows - 1 go to part_o and part_ml.
@@ -451,7 +490,10 @@ __device__ void attend(const PrefixArgs& a, typename Run<T, DP, CT, NC>::Lds& ld
       lds.join.m[g][tid] = f;
     }
     if (tid < rows) *(float2*)(part_ml + 2 * tid) = make_float2(mm, ll);
+    lds.join.l[0][tid] = mm;
   }
+  __shared__ unsigned long long spoilt;  // rows with a sum that is not finite
+  if (tid == 0) spoilt = 0;
   lds_barrier();
   constexpr int kRow = DP / 4;  // threads of a row
   const int d = tid % kRow * 4;
@@ -461,7 +503,16 @@ __device__ void attend(const PrefixArgs& a, typename Run<T, DP, CT, NC>::Lds& ld
 #pragma unroll
       for (int g = 0; g < R::NG; ++g) acc += lds.join.m[g][r] * *(const f4*)&lds.join.o[g][r][d];
       *(f4*)(part_o + (int64_t)r * a.D + d) = acc;
+      if (!(fabsf(acc[0] + acc[1] + acc[2] + acc[3]) < INFINITY)) atomicOr(&spoilt, 1ull << r);
     }
+  __syncthreads();
+  if (spoilt == 0) return;
+  for (int r = wave; r < rows; r += kWaves) {
+    const int end = limit_of(r);
+    if ((spoilt >> r & 1) && end < k1)  // (what a row attends whole is its own)
+      own_sum<T, DP>(a, table, kc, vc, row_of(r), k0, end, lds.join.l[0][r],
+                     part_o + (int64_t)r * a.D);
+  }
 }
 
 // Row tiles of the prefix, 16 CT NC rows each: query r of a key head is head r % G of

@@ -81,3 +81,45 @@ def test_nan_key_of_the_prefix(token, dtype):
     touched = rows_of(out)
     touched[np.array(shared) > token, :4] = True
     check_others(out, want, touched)
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("D", [40, 64, 128, 256])
+@pytest.mark.parametrize("Hq,H", [(4, 2), (12, 2), (34, 2)])
+@pytest.mark.parametrize("value", [NAN, INF, -INF])
+def test_values_of_keys_of_other_sequences(value, Hq, H, D, dtype):
+    """The prefix's keys and values, and the own ones of other sequences, past what a
+    sequence shares, whatever they hold: sequences that end before, inside and behind the
+    tiles and runs where they lie."""
+    shared = [300, 170, 0, 131, 130, 129, 64, 300, 1, 170]
+    lengths = [300, 180, 20, 131, 200, 129, 64, 340, 1, 170]
+    a = make(shared, lengths, Hq, H, D, 16, dtype, prefix=300, seed=D)
+    want = plain(*a)
+    q, cache, table, _, ptab, _ = a
+    touched = np.zeros(q.shape, bool)
+    G = Hq // H
+    for token, head, d in ((130, 0, 3), (131, 1, D - 1), (171, 0, 0), (250, 1, 8)):
+        cache.v[int(ptab[token // 16]), token % 16, head, d] = value
+        touched[np.array(shared) > token, head * G:(head + 1) * G, d] = True
+    cache.v[int(table[7, 310 // 16]), 310 % 16, 0, 5] = value
+    touched[7, :G, 5] = True
+    check_others(api.attn_prefix(*a), want, touched)
+    # keys too: NaN scores for those who attend them
+    cache.k[int(ptab[180 // 16]), 180 % 16, 1, 2] = NAN
+    touched[np.array(shared) > 180, G:] = True
+    check_others(api.attn_prefix(*a), want, touched)
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+def test_sequences_without_a_share_beside_a_prefix_of_nan(dtype):
+    shared = [200, 0, 200, 0, 0]
+    a = make(shared, [200, 50, 210, 1, 0], 8, 2, 128, 16, dtype, seed=1)
+    want = plain(*a)
+    cache, ptab = a[1], a[4]
+    cache.k[ptab.long()] = NAN
+    cache.v[ptab.long()] = NAN
+    out = api.attn_prefix(*a)
+    touched = rows_of(out)
+    touched[[0, 2]] = True
+    check_others(out, want, touched)
+    assert (out[4] == 0).all()
