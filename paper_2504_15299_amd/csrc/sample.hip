@@ -765,13 +765,29 @@ __global__ __launch_bounds__(kThreads) void sample_kernel(SampleArgs a) {
   }
 }
 
+constexpr int kMostRows = 1 << 21;  // of a launch, whose threads must be fewer than 2^32
+
 // Rows of up to 16 times 16 bytes a thread are held.
 template <typename T>
-void run_sample(const SampleArgs& a, int B, hipStream_t s) {
-  if (a.V <= RowOf<T>::HELD * kThreads * RowOf<T>::PER)
-    sample_kernel<T, true><<<B, kThreads, 0, s>>>(a);
-  else
-    sample_kernel<T, false><<<B, kThreads, 0, s>>>(a);
+hipError_t run_sample(SampleArgs a, int B, hipStream_t s) {
+  for (;;) {
+    const int n = B < kMostRows ? B : kMostRows;
+    if (a.V <= RowOf<T>::HELD * kThreads * RowOf<T>::PER)
+      sample_kernel<T, true><<<n, kThreads, 0, s>>>(a);
+    else
+      sample_kernel<T, false><<<n, kThreads, 0, s>>>(a);
+    const hipError_t err = hipGetLastError();
+    B -= n;
+    if (err != hipSuccess || B == 0) return err;
+    a.logits = (const T*)a.logits + n * a.stride;
+    a.u += n;
+    if (a.temperature) a.temperature += n;
+    if (a.top_k) a.top_k += n;
+    if (a.top_p) a.top_p += n;
+    if (a.min_p) a.min_p += n;
+    a.tokens += n;
+    if (a.probs) a.probs += n;
+  }
 }
 
 }  // namespace
@@ -783,13 +799,9 @@ hipError_t launch_sample(const void* logits, d2moe_dtype dtype, int64_t stride, 
   if (B == 0) return hipSuccess;
   int bits = 0;
   while ((1 << bits) < V) ++bits;
-  SampleArgs a{logits, stride, V, 62 - bits < 51 ? 62 - bits : 51, u, temperature, top_k, top_p,
-               min_p, tokens, probs};
-  if (dtype == D2MOE_BF16)
-    run_sample<uint16_t>(a, B, s);
-  else
-    run_sample<float>(a, B, s);
-  return hipGetLastError();
+  const SampleArgs a{logits, stride, V,     62 - bits < 51 ? 62 - bits : 51, u, temperature,
+                     top_k,  top_p,  min_p, tokens, probs};
+  return dtype == D2MOE_BF16 ? run_sample<uint16_t>(a, B, s) : run_sample<float>(a, B, s);
 }
 
 }  // namespace d2moe

@@ -8,7 +8,7 @@ import torch
 
 from layer_cases import DEV
 from paper_2504_15299_amd import api
-from test_gpu_sample import BF, F32, gpu, normal, run
+from test_gpu_sample import BF, F32, I32, gpu, normal, run
 
 pytestmark = pytest.mark.gpu
 
@@ -103,3 +103,19 @@ def test_tokens_of_the_least_weights(mask, p):
     for token, share in zip(tokens, probs):
         want = (1.0 if token == first else w) / kept
         assert abs(share - want) <= (2.0 ** -24 + 2.0 ** -14) * want
+
+
+@pytest.mark.parametrize("dtype", [F32, BF])
+def test_rows_of_more_than_one_launch(dtype):
+    """More rows than one launch has threads for, each with settings of its own."""
+    B, V = (1 << 22) + 3, 3
+    x = torch.zeros((B, V), dtype=dtype, device=DEV)
+    i = torch.arange(B, device=DEV)
+    u = (i % 8).float() / 8
+    k = (i % 4).to(I32)                 # 0: all three
+    t = (i % 5 > 0).float()             # 0: the first
+    tokens, probs = api.sample(x, u, temperature=t, top_k=k)
+    n = torch.where(k == 0, 3, k.long())
+    n = torch.where(t == 0, 1, n)
+    assert torch.equal(tokens.long(), (u.double() * n).floor().long())
+    assert torch.equal(probs, (1.0 / n.double()).float())
