@@ -24,6 +24,7 @@ constexpr int kMaxKeys = 64 * 8;   // E <= 64, L <= 8
 constexpr int kBlock = 1024;       // slots of a block, one a thread; the last one's up to twice
 constexpr int kOneTokens = 64;     // tokens that one workgroup chooses for
 constexpr int kOneSlots = 2 * kBlock - 1;  // slots that one workgroup places
+constexpr int kMostTokens = 1 << 24;  // of a launch, whose threads must be fewer than 2^32
 static_assert(kBlock > kMaxKeys, "a block's table fits its part of slot_of");
 
 struct ScoredArgs {
@@ -168,11 +169,11 @@ __device__ int select(const ScoredArgs& a, int t, int lane, double (&tmp)[64], i
   return flag;
 }
 
-// Many tokens: one wave each; the flag bits wait in perm[t].
-__global__ __launch_bounds__(256) void scored_select_kernel(ScoredArgs a) {
+// Many tokens, from `first` on: one wave each; the flag bits wait in perm[t].
+__global__ __launch_bounds__(256) void scored_select_kernel(ScoredArgs a, int first) {
   __shared__ double tmp[4][64];
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
-  const int t = blockIdx.x * 4 + wave;
+  const int t = first + blockIdx.x * 4 + wave;
   if (t >= a.T) return;
   const int flag = select(a, t, lane, tmp[wave], nullptr);
   if (lane == 0) a.perm[t] = flag;
@@ -369,8 +370,11 @@ hipError_t launch_route_scored(const void* x, d2moe_dtype xd, int T, int d, cons
                                float scale, const int32_t* token_req, const uint8_t* bit_table,
                                int R, int b_min, int b_max, const d2moe_routing* out,
                                hipStream_t s) {
-  if (x && T > 0) {
-    const hipError_t err = launch_gate(x, xd, T, d, Wg, bias, E, out->logits, s);
+  const size_t row = (size_t)d * (xd == D2MOE_BF16 ? 2 : 4);
+  for (int t = 0; x && t < T; t += kMostTokens) {
+    const hipError_t err =
+        launch_gate((const char*)x + t * row, xd, T - t < kMostTokens ? T - t : kMostTokens, d, Wg,
+                    bias, E, out->logits + (int64_t)t * E, s);
     if (err != hipSuccess) return err;
   }
   ScoredArgs a{};
@@ -385,9 +389,12 @@ hipError_t launch_route_scored(const void* x, d2moe_dtype xd, int T, int d, cons
     scored_one_kernel<true><<<1, kThreads, 0, s>>>(a);
     return hipGetLastError();
   }
-  scored_select_kernel<<<(T + 3) / 4, 256, 0, s>>>(a);
-  hipError_t err = hipGetLastError();
-  if (err != hipSuccess) return err;
+  hipError_t err;
+  for (int t = 0; t < T; t += kMostTokens) {
+    const int n = T - t < kMostTokens ? T - t : kMostTokens;
+    scored_select_kernel<<<(n + 3) / 4, 256, 0, s>>>(a, t);
+    if ((err = hipGetLastError()) != hipSuccess) return err;
+  }
   if (n <= kOneSlots) {
     scored_one_kernel<false><<<1, kThreads, 0, s>>>(a);
     return hipGetLastError();
