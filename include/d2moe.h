@@ -647,9 +647,9 @@ d2moe_status d2moe_attn_decode(const void* q, int64_t q_stride, int32_t B, int32
  *        ones count as 0, ones beyond the prefix's table as its end
  *   max_prefix, max_rest: host, the largest s and n - s expected; only the division of
  *        the work goes by them, any lengths give their result; at most 2^30
- *   workspace: at least d2moe_attn_prefix_workspace bytes for these two (no fewer for
- *        larger ones), 16-byte aligned; contents need no initialisation; calls that may
- *        run at the same time need one each
+ *   workspace: at least d2moe_attn_prefix_workspace bytes for these two and this B (no
+ *        fewer for larger ones), 16-byte aligned; contents need no initialisation; calls
+ *        that may run at the same time need one each
  *   out: packed; may begin where q does, whatever q's stride
  * Everything else as d2moe_attn_decode without a window: lengths, masked tokens, rows
  * without a key, types, sums and limits (also prefix_pages * page_size <= 2^30).  An

@@ -802,6 +802,15 @@ void divide(int keys, int64_t units, int groups, int least, int& splits, int& ch
   if (chunk < least) chunk = least;
 }
 
+// No fewer runs than divide() makes of this many units or fewer: fewer units are cut into
+// more runs each, and a workspace for the largest batch is to serve every smaller one.
+int64_t most_runs(int keys, int64_t units, int groups, int least) {
+  int64_t splits = ((int64_t)keys + least - 1) / least;
+  splits = splits < 1 ? 1 : splits < kMostSplits ? splits : kMostSplits;
+  const int64_t runs = units * splits < groups ? units * splits : groups;
+  return runs > units ? runs : units;
+}
+
 Plan plan_of(int B, int q_heads, int n_heads, int max_prefix, int max_rest) {
   Plan p;
   const int G = q_heads / n_heads, rows = B * G;
@@ -850,8 +859,12 @@ size_t attn_prefix_workspace(int B, int q_heads, int n_heads, int dim, int max_p
                              int max_rest) {
   if (B == 0) return 0;
   const Plan p = plan_of(B, q_heads, n_heads, max_prefix, max_rest);
-  return (size_t)(shared_rows(p, n_heads) + own_rows(p, B, q_heads, n_heads)) * (dim + 2) *
-         sizeof(float);
+  const int G = q_heads / n_heads;
+  const int64_t tiles = (int64_t)n_heads * p.row_tiles;
+  const int64_t own = (int64_t)n_heads * p.head_tiles * B;
+  return (size_t)(most_runs(max_prefix, tiles, kSharedGroups, kLeastKeys) * p.tile_rows +
+                  most_runs(max_rest, own, kOwnRuns, kLeastOwn) * (G < kRows ? G : kRows)) *
+         (dim + 2) * sizeof(float);
 }
 
 hipError_t launch_attn_prefix(const void* q, int64_t q_stride, int B, int q_heads,
