@@ -705,9 +705,10 @@ d2moe_status d2moe_block_norm(float* x, float x_scale, const void* y, d2moe_dtyp
  *   tokens: device [B] int32; probs: device [B] float or NULL, the token's share of the
  *        kept sum (1 with temperature 0)
  * Tokens of logit -infinity or NaN are never chosen; a row of nothing else gives token
- * -1 with share 0.  Logits of +infinity share the whole.  Weights are binary64, rounded
- * to multiples of 2^-(62 - ceil(log2 V)) (2^-51 at most), whose sums are exact: the result
- * does not depend on what else runs, and tokens of less than half a unit are not drawn.
+ * -1 with share 0.  Logits of +infinity share the whole.  Weights are within 2^-42 of
+ * themselves, then rounded to multiples of 2^-(62 - ceil(log2 V)) (2^-51 at most), whose
+ * sums are exact: the result does not depend on what else runs, and tokens of less than
+ * half a unit are not drawn.
  * 1 <= V <= 2^24, B <= 2^24.
  */
 d2moe_status d2moe_sample(const void* logits, d2moe_dtype dtype, int64_t stride, int32_t B,

@@ -14,9 +14,10 @@
 // one workgroup a CU; 16 behind 2000 15; 2 of 40 behind 501 9).  A step of 64 shared keys
 // and 64 rows takes 4600 cycles, of which 1000 are matrix products, 1800 with the reads
 // and turns of the values, 1300 the loads and the scores, 600 the exponents, 900 the
-// stores and barriers: two waves a SIMD are all that the registers hold.  Own tokens by
-// whole workgroups, four waves to a run, joined in LDS, took 23.3 us for 20.4, and 52 for
-// 32 where many have few (114 sequences of up to 39, 64 and 8 heads of 256).
+// stores and barriers, one after the other in the one wave of the prefix that a SIMD has;
+// the registers hold one more, which has own tokens.  Own tokens by whole workgroups, four
+// waves to a run, joined in LDS, took 23.3 us for 20.4, and 52 for 32 where many have few
+// (114 sequences of up to 39, 64 and 8 heads of 256).
 //
 // As in the attention of single sequences,
 //   S (keys x queries) = K Q^T,   O^T (values x queries) = V^T P^T
@@ -289,7 +290,8 @@ struct Run {
 // One row's value sum by a wave, a key after the other and only those that it attends.  In
 // the matrix products 0 times an infinite or NaN value is not 0, so that such a value
 // reaches the rows of a tile that do not attend its key as well: seldom, and their sums are
-// made here once more.
+// made here once more (64 sequences behind 8192 tokens, a fourth of them sharing 4000, with
+// an infinite value further on: 48.4 us, without one 43.0).
 __device__ inline float value_of(const uint16_t* p) { return bf2f(*p); }
 __device__ inline float value_of(const float* p) { return *p; }
 template <typename T, int DP>
@@ -783,11 +785,12 @@ struct Plan {
 };
 // Runs that the keys are cut into: of the prefix's one a CU (64 sequences behind 8192
 // keys 44 us, with 128 of them 64, with 512 48; the other way without own tokens, 40 and
-// 36), of the own tokens eight a CU (64 sequences of up to 512, 12 heads of 64 in fp32: 30.0
-// us, with 1024 of them 37.4; 4096 take 22.7 for 20.4 with 32 and 8 heads of 128 in bf16);
-// and the least keys of a run (of the prefix: 16 sequences behind 2000 15.6 us, with 64
-// 19.1, with 256 16.6; of the own tokens: 9 of 300 behind 1500, fp32, 10.9 us, with 128
-// 13.9; 32 of 300 with heads of 256 47.5, with 32 53.6).
+// 36; 129 to 255 units are one run each, which leaves CUs without one), of the own tokens
+// eight a CU (64 sequences of up to 512, 12 heads of 64 in fp32: 30.0 us, with 1024 of them
+// 37.4; 4096 take 22.7 for 20.4 with 32 and 8 heads of 128 in bf16); and the least keys of a
+// run (of the prefix: 16 sequences behind 2000 15.6 us, with 64 19.1, with 256 16.6; of the
+// own tokens: 9 of 300 behind 1500, fp32, 10.9 us, with 128 13.9; 32 of 300 with heads of
+// 256 47.5, with 32 53.6).
 constexpr int kSharedGroups = 256, kOwnRuns = 2048;
 constexpr int kLeastKeys = 128, kLeastOwn = 64;
 constexpr int kMostSplits = 64;

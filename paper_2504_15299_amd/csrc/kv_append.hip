@@ -144,9 +144,11 @@ hipError_t run_append(const AppendArgs& a, hipStream_t s) {
 // Memory-bound: 8192 tokens of 32 and 8 heads of 128, bf16, take 42.5 us, 4.7 TB/s (a
 // scaled copy of as many bytes 37.5); 16 tokens 3.5 us, which is latency.  The heads'
 // loads are under way before the token's position is waited for (one after the other:
-// 52 us), and the 5 workgroups a compute unit that the registers leave room for go over
-// the tokens (6: 48.5 us, 7: 45.4, one for each 4 waves' work 47).  Two of a wave's
-// heads in flight at once gain nothing (46 us).
+// 52 us), rows are stored past the caches (through them 48 us and more; 16 tokens and the
+// attention that reads them next 20.1 us, through them 19.9, 256 tokens 189 for 192), and
+// the 5 workgroups a compute unit that the registers leave room for go over the tokens (6:
+// 48.5 us, 7: 45.4, one for each 4 waves' work 47).  Two of a wave's heads in flight at once
+// gain nothing (46 us).
 struct NormArgs {
   AppendArgs a;
   const float *qw, *kw;  // [D] or null

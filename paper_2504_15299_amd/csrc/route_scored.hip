@@ -8,10 +8,14 @@
 // order, the upper words first (as binary64, 8192 tokens' choices take 11.6 us for 9.3).
 //
 // Up to kOneTokens tokens everything is one workgroup (16 tokens, 2 of 8 experts: 6.0
-// us, latency: a load, the scores, the k maxima and seven barriers).  Above, a wave a
-// token chooses, then every kBlock slots are counted, each key's counts scanned over the
-// blocks, and the slots placed; the tables between the launches lie in the part of
-// slot_of that their block writes last.  8192 tokens, 6 of 64 experts in 4 of 8 groups,
+// us, latency: a load, the scores, the k maxima and seven barriers).  A wave then has up to
+// four tokens one after the other, for a launch less, which counts where calls follow each
+// other: 64 tokens, 2 of 8 experts, 12.3 us a call for 12.8 of two launches; 6 of 64 experts
+// 9.7 at 32 tokens, 15.1 at 64, for 12.8.  (In a captured graph two are faster from 17 tokens
+// on: at 16, 32 and 64 tokens, 6 of 64 experts, 7.4, 9.9 and 15.4 us, two 7.8, 7.7 and 8.0.)
+// Above, a wave a token chooses, then every kBlock slots are counted, each key's counts
+// scanned over the blocks, and the slots placed (up to kOneSlots by one workgroup); the
+// tables between the launches lie in the part of slot_of that their block writes last.  8192 tokens, 6 of 64 experts in 4 of 8 groups,
 // sigmoid: 9.3 + 2.8 + 3.0 + 4.8 us, the choice bound by its instructions (3 MB cross
 // the memory, 0.6 us), the others by latency.
 #include "internal.h"

@@ -16,13 +16,12 @@
 // in 64 bits (2^-47 at 32000 tokens).  Their sums are exact, so that no order of
 // additions turns a choice; a token below half a unit is never drawn.
 //
-// Bound by the instructions of the one CU that has a row: about 25 a token for its
-// weight, 20 more for the histogram, 5 for a list.  (One row of 32000 in binary32 with
-// top-p: 21.7 us, of which 9 in the histogram; 256 of 131072 in bf16 with all bounds:
-// 71 to 75 us, reading them alone 11; the rows without top-k take longest, 37 us of it for the
-// histogram's pass, one over four loads ahead no less.)  512 threads a row were slower,
-// 27 and 96 us.
-//
+// Bound by the instructions of the one CU that has a row: 28 a token for its weight in a
+// sum, 36 with its bin, 5 for a list.  (One row of 32000 in binary32 with top-p: 20 to 23
+// us, by what the settings leave, of which 9 in the histogram; 256 of 131072 in bf16 with
+// all bounds: 71 to 75 us, reading them alone 11; the rows without top-k take longest, 37 us
+// of it for the histogram's pass, one over four loads ahead no less.)  512 threads a row
+// were slower, 27 and 96 us.
 #include <cfloat>
 
 #include "decoder.h"

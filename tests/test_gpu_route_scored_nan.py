@@ -30,7 +30,8 @@ def test_rows_without_a_finite_logit(T, renorm, scoring):
     assert idx.tolist() == [list(range(8)), [0, 2, 3, 4, 6, 7, 1, 5], list(range(8))]
     assert np.isnan(w[0]).all() and (w[2] == 0).all()
     # (a sum with a NaN in it is one)
-    assert np.isnan(w[1, 6:]).all() and (np.isnan(w[1, :6]).all() if renorm else (w[1, :6] == 0).all())
+    assert np.isnan(w[1, 6:]).all()
+    assert (np.isnan(w[1, :6]) if renorm else w[1, :6] == 0).all()
 
 
 @pytest.mark.parametrize("T", [4, 100])

@@ -13,8 +13,10 @@ def need(*a):
     return n.value
 
 
-@pytest.mark.parametrize("heads", [(32, 8, 128), (12, 12, 64), (34, 2, 256), (1, 1, 8), (64, 1, 128)])
-@pytest.mark.parametrize("lengths", [(8192, 512), (8192, 0), (0, 5000), (129, 65), (1 << 30, 1 << 30)])
+@pytest.mark.parametrize("heads", [(32, 8, 128), (12, 12, 64), (34, 2, 256), (1, 1, 8),
+                                   (64, 1, 128)])
+@pytest.mark.parametrize("lengths", [(8192, 512), (8192, 0), (0, 5000), (129, 65),
+                                     (1 << 30, 1 << 30)])
 def test_grows_with_the_batch(heads, lengths):
     last = 0
     for B in list(range(1, 700)) + list(range(700, 65000, 331)):
