@@ -15,9 +15,9 @@
 // on: at 16, 32 and 64 tokens, 6 of 64 experts, 7.4, 9.9 and 15.4 us, two 7.8, 7.7 and 8.0.)
 // Above, a wave a token chooses, then every kBlock slots are counted, each key's counts
 // scanned over the blocks, and the slots placed (up to kOneSlots by one workgroup); the
-// tables between the launches lie in the part of slot_of that their block writes last.  8192 tokens, 6 of 64 experts in 4 of 8 groups,
-// sigmoid: 9.3 + 2.8 + 3.0 + 4.8 us, the choice bound by its instructions (3 MB cross
-// the memory, 0.6 us), the others by latency.
+// tables between the launches lie in the part of slot_of that their block writes last.  8192
+// tokens, 6 of 64 experts in 4 of 8 groups, sigmoid: 9.6 + 2.7 + 3.1 + 4.8 us, the choice
+// bound by its instructions (3 MB cross the memory, 0.6 us), the others by latency.
 #include "internal.h"
 
 namespace d2moe {
